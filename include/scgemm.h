@@ -83,7 +83,9 @@ enum {
     SC_ERR_HIP = -7,           /* a HIP runtime call or kernel launch failed */
     SC_ERR_DEVICE_STATUS = -8, /* (sc_gemm_status) some L_i was outside [0, L_max] */
     SC_ERR_STRIDE = -9,        /* a row stride is smaller than the row length */
-    SC_ERR_RESERVED = -10      /* the descriptor's reserved field is not 0 */
+    SC_ERR_RESERVED = -10,     /* the descriptor's reserved field is not 0 */
+    SC_ERR_TYPE = -11          /* an element type, block, norm or pairing that is not one of its
+                                  list, or not served there (layer operators below) */
 };
 
 enum { SC_BIPOLAR_XNOR = 0, SC_UNIPOLAR_AND_SM = 1 };
@@ -226,6 +228,180 @@ int sc_quantize(int32_t batch, int32_t rows, int32_t K, const float *X, int64_t 
 int sc_mp_lengths(int32_t batch, int32_t M, const float *metric, int64_t strideM,
                   const float *tau, const int32_t *ladder, int32_t n_levels, int32_t *L_out,
                   int64_t strideL, void *stream);
+
+/*
+ * ------------------------------------------------------------------------------------
+ * Layer operators around the quantised products: 8-bit float products with block scales,
+ * the norms, gate and residual between two branches of a transformer block, and rotary
+ * positions.  They share sc_gemm's conventions: device pointers, strides in elements,
+ * asynchronous on `stream`, arguments checked on the host before anything is enqueued, no
+ * allocation, no state between calls.  Every stride is at least 0; the last dimension is
+ * contiguous; sizes of 0 are allowed and write nothing (or zeros, where said).  No pointer
+ * needs more than its element's alignment (16-byte aligned rows are faster).  Outputs must
+ * not overlap inputs unless said.
+ */
+enum { SC_F32 = 0, SC_BF16 = 1, SC_F16 = 2, SC_E4M3 = 3, SC_E5M2 = 4, SC_INT8 = 5 };
+
+#define SC_FP8_BLOCK 128
+
+/* Blocks of sc_fp8_quantize. */
+enum {
+    SC_BLOCK_1X128 = 0,    /* 128 neighbours of a row */
+    SC_BLOCK_128X128 = 1,  /* 128 rows x 128 columns */
+    SC_BLOCK_128X1_T = 2   /* 128 rows of a column; Q and scale leave transposed */
+};
+
+/*
+ * 8-bit floats with an fp32 scale for each block: for a block with m = max |x| (NaN passed over)
+ *   s = 0 where m = 0, else max(m / top, 2^-126), top = 448 (SC_E4M3) or 57344 (SC_E5M2)
+ *   Q = the nearest 8-bit float (ties to even) of x * (1 / s), held within [-top, top]
+ * in IEEE fp32, so the result is bit-identical to the same formula on the host.  A NaN stays NaN; an
+ * infinite element gives an infinite scale and NaN for itself.  Blocks at the ends of rows and columns
+ * are cut short.
+ *   X      typeX (SC_F32, SC_BF16, SC_F16)  X[b*strideX + i*ldx + d], rows x K
+ *   Q      typeQ   Q[b*strideQ + i*ldq + d]; SC_BLOCK_128X1_T: Q[b*strideQ + d*ldq + i]
+ *   scale  fp32    SC_BLOCK_1X128:   scale[b*strideS + i*lds + d/128]
+ *                  SC_BLOCK_128X128: scale[b*strideS + (i/128)*lds + d/128]
+ *                  SC_BLOCK_128X1_T: scale[b*strideS + d*lds + i/128]
+ * These are the operands of sc_fp8_gemm.  K <= SC_K_LIMIT.
+ */
+int sc_fp8_quantize(int32_t batch, int32_t rows, int32_t K, int32_t typeX, const void *X, int64_t ldx,
+                    int64_t strideX, int32_t typeQ, int32_t block, void *Q, int64_t ldq, int64_t strideQ,
+                    float *scale, int64_t lds, int64_t strideS, void *stream);
+
+typedef struct sc_fp8_gemm_desc {
+    int32_t batch;              /* >= 0 independent problems */
+    int32_t M, N, K;            /* A[b] is M x K, B[b] is N x K, out[b] is M x N */
+    int64_t lda, ldb, ldo;      /* row strides in elements (>= K, >= K, >= N) */
+    int64_t strideA, strideB, strideO;      /* batch strides; 0 = broadcast (A, B) */
+    int64_t ldsA, ldsB;         /* row strides of the scales (>= ceil(K / 128)) */
+    int64_t strideSA, strideSB; /* batch strides of the scales */
+    int64_t strideBias;         /* batch stride of bias (N); 0 = shared */
+    int32_t typeA, typeB;       /* SC_E4M3 or SC_E5M2 each */
+    int32_t rowsA, rowsB;       /* rows that share a scale: 1 or 128 */
+    int32_t typeO;              /* SC_F32, SC_BF16 or SC_F16 */
+    int32_t reserved;           /* must be 0 */
+} sc_fp8_gemm_desc;
+
+/* Bytes of device workspace sc_fp8_gemm needs for `desc` on the current device (may be 0). */
+int sc_fp8_gemm_workspace_size(const sc_fp8_gemm_desc *desc, size_t *bytes);
+
+/*
+ * Product of 8-bit floats whose rows have a scale for each block of 128 elements:
+ *   out_ij = sum_t sA[i/rowsA, t] sB[j/rowsB, t] sum_{d in block t} A_id B_jd  (+ bias_j)
+ * rounded once to typeO (ties to even).  Scales, sums over blocks and the bias are in fp32.  typeO SC_F32: so are the
+ * products and sums inside a block.  SC_BF16, SC_F16: inside a block the matrix cores' 8-bit products, of which each
+ * eight neighbours keep what lies within 2^-13 of the largest one's power of two, are summed in fp32.
+ *   A, B   8-bit floats   A[b*strideA + i*lda + d], B[b*strideB + j*ldb + d]
+ *   sA     fp32           sA[b*strideSA + (i/rowsA)*ldsA + t], sB alike
+ *   bias   fp32           bias[b*strideBias + j], NULLABLE
+ *   out    typeO          out[b*strideO + i*ldo + j]   (written; K = 0 gives the bias, or 0)
+ *   workspace             as sc_gemm's; NULL where sc_fp8_gemm_workspace_size gives 0
+ * The order of the sums depends on the sizes alone: same call, same bits.
+ */
+int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, const void *B, const float *sB,
+                const float *bias, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+enum { SC_NORM_NONE = 0, SC_NORM_RMS = 1, SC_NORM_LAYER = 2 };
+
+#define SC_NORM_D_LIMIT 16384            /* longest row of the norms */
+
+typedef struct sc_norm_desc {
+    int32_t batch, rows, D;     /* rows x D elements in each of batch entries; D <= SC_NORM_D_LIMIT */
+    int32_t post, pre;          /* SC_NORM_*: the norm behind the branch, the norm before the next */
+    int32_t typeX, typeY;       /* residual stream and branch: SC_F32, SC_BF16 or SC_F16 */
+    int32_t typeP;              /* parameters: SC_F32, SC_BF16 or SC_F16 */
+    int32_t typeH;              /* h: SC_F32, SC_BF16, SC_F16; forward also SC_INT8, SC_E4M3, SC_E5M2 */
+    float eps_post, eps_pre;    /* > 0 */
+    float scale_res;            /* factor of the residual stream */
+    float off_post, off_pre;    /* added to the norms' weights (1 where the parameter is 1 + w) */
+    int32_t reserved;           /* must be 0 */
+    int64_t ldx, strideX;       /* x (backward: dx): element i, d of entry b at b*strideX + i*ldx + d */
+    int64_t ldy, strideY;       /* y */
+    int64_t ldxo, strideXO;     /* xo */
+    int64_t ldh, strideH;       /* h (backward: dh) */
+    int64_t lds, strideS;       /* scales of a quantised h: row and batch stride (see below) */
+    int64_t lddxo, strideDXO;   /* dxo (backward only) */
+    int64_t lddy, strideDY;     /* dy (backward only) */
+    int64_t stride_post_w, stride_post_b, stride_gate, stride_pre_w, stride_pre_b;
+                                /* batch strides of the parameters (D each); 0 = shared */
+} sc_norm_desc;
+
+/*
+ * The seam between two branches of a transformer block: the norm behind the branch y, its gate, the
+ * residual and the norm before the next branch, row by row in fp32:
+ *   u  = n_post(y) (off_post + post_w) + post_b     (SC_NORM_NONE: u = y, post_w and post_b NULL)
+ *   xo = scale_res x + gate u                       (rounded to typeX where it is stored)
+ *   h  = n_pre(xo) (off_pre + pre_w) + pre_b        (of xo before that rounding; SC_NORM_NONE: h = xo)
+ *   SC_NORM_RMS:   n(v) = v / sqrt(mean(v^2) + eps)
+ *   SC_NORM_LAYER: n(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps)
+ * A parameter that is NULL leaves its factor at 1 (gate, off + w) or its term at 0.  Parameters of a
+ * batch entry (adaptive norms: shift, scale and gate per image) have a batch stride, shared ones 0.
+ *   x         typeX (read)      y   typeY (read), NULLABLE: no branch, xo = scale_res x
+ *   xo        typeX, NULLABLE (written); may be x itself with x's strides
+ *   h         typeH, NULLABLE (written); SC_NORM_NONE with SC_INT8 or an fp8 type only quantises
+ *   SC_INT8   h = int8 rows, scale[b*strideS + i] and rowmax[b*strideS + i] (NULLABLE) as sc_quantize
+ *             makes them of the fp32 h: operands of sc_gemm and the metric of sc_mp_lengths
+ *   SC_E4M3, SC_E5M2   h and scale[b*strideS + i*lds + d/128] as sc_fp8_quantize makes them of the
+ *             fp32 h with SC_BLOCK_1X128: operands of sc_fp8_gemm; rowmax NULL
+ */
+int sc_residual_norm(const sc_norm_desc *desc, const void *x, const void *y, const void *post_w,
+                     const void *post_b, const void *gate, const void *pre_w, const void *pre_b, void *xo,
+                     void *h, float *scale, float *rowmax, void *stream);
+
+/* Bytes of device workspace sc_residual_norm_backward needs (partial sums of the parameters' gradients). */
+int sc_residual_norm_backward_workspace_size(const sc_norm_desc *desc, size_t *bytes);
+
+/*
+ * Gradients of sc_residual_norm from those of its outputs (dxo of xo, dh of h; NULL = zero).  xo (as the
+ * forward pass stored it) and y are read again, and the norms' statistics are computed from them.  typeH is the
+ * type of dh and a float type.
+ *   dx        typeX, NULLABLE (written); may be dxo itself with dxo's strides
+ *   dy        typeY, NULLABLE (written)
+ *   dpost_w, dpost_b, dgate, dpre_w, dpre_b   fp32, NULLABLE (written): the parameter's gradient, [b*D + d], or
+ *             [d] summed over the batch too where the parameter's batch stride is 0
+ * xo may be NULL where pre is SC_NORM_NONE and neither dpre_w nor dpre_b is wanted; y where post is SC_NORM_NONE and
+ * neither dgate nor a post gradient is wanted.  The sums' order depends on the sizes alone: same call, same bits.
+ */
+int sc_residual_norm_backward(const sc_norm_desc *desc, const void *xo, const void *y, const void *post_w,
+                              const void *post_b, const void *gate, const void *pre_w, const void *dxo,
+                              const void *dh, void *dx, void *dy, float *dpost_w, float *dpost_b,
+                              float *dgate, float *dpre_w, float *dpre_b, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+enum { SC_ROPE_HALVES = 0, SC_ROPE_NEIGHBOURS = 1 };
+
+typedef struct sc_rope_desc {
+    int32_t batch, tokens, heads, D;   /* x[b] is tokens x heads x D; D <= SC_ROPE_D_LIMIT */
+    int32_t pairs, axes;        /* the first 2 * pairs elements turn (2 * pairs <= D); 1..SC_ROPE_AXES_LIMIT axes */
+    int32_t pairing;            /* SC_ROPE_HALVES: pair p is elements p and pairs + p; SC_ROPE_NEIGHBOURS: 2p and 2p + 1 */
+    int32_t inverse;            /* 0, or 1: turn back (the gradient) */
+    int32_t typeX, typeO;       /* SC_F32, SC_BF16, SC_F16; typeO also SC_INT8 */
+    int32_t reserved[2];        /* must be 0 */
+    int64_t strideXB, strideXT, strideXH;   /* strides of x over batch, tokens and heads */
+    int64_t strideOB, strideOT, strideOH;   /* of out */
+    int64_t strideSB, strideST, strideSH;   /* of scale and rowmax (SC_INT8) */
+    int64_t stridePB, stridePA; /* of positions over batch (0 = shared) and axes; tokens are neighbours */
+} sc_rope_desc;
+
+#define SC_ROPE_D_LIMIT 256
+#define SC_ROPE_AXES_LIMIT 8
+
+/*
+ * Rotary positions with several axes (time, height, width): pair p of token t turns by the angle
+ *   a = pos[b*stridePB + axis[p]*stridePA + t] * freq[p]
+ *   (u, v) -> (u cos a - v sin a, u sin a + v cos a);  inverse: by -a
+ * and the elements behind the last pair pass unchanged.  The angle is formed and reduced in twice
+ * 64 bits, so that far positions lose nothing; the turn is in fp32, rounded once to typeO.
+ *   x     typeX
+ *   pos   int32, any value       freq  fp64, pairs of them       axis  int32, pairs of them, all DEVICE arrays;
+ *         a pair whose axis is outside [0, axes) does not turn
+ *   out   typeO; may be x itself with x's strides and type
+ *   SC_INT8: out = int8 rows of D elements with scale[b*strideSB + t*strideST + h*strideSH] and rowmax (NULLABLE)
+ *         as sc_quantize makes them of the fp32 result: head by head, an operand of sc_gemm
+ */
+int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *pos, const double *freq, const int32_t *axis,
+            void *out, float *scale, float *rowmax, void *stream);
 
 /* Human-readable name of a status code (static string). */
 const char *sc_strerror(int code);

@@ -17,7 +17,12 @@ from ._lib import (SC_BIPOLAR_XNOR, SC_ERR_DEVICE_STATUS, SC_ERR_RESERVED, SC_KL
 __all__ = ["gemm", "make_desc", "comparator_sequence", "quantize", "mp_lengths", "Workspace",
            "ScGemmDesc", "ScError", "sc_gemm", "sc_gemm_noalloc", "sc_gemm_workspace_size", "sc_gemm_status",
            "sc_comparator_sequence", "sc_quantize", "sc_mp_lengths", "SC_BIPOLAR_XNOR",
-           "SC_UNIPOLAR_AND_SM", "SC_RNG_LFSR32", "SC_RNG_SOBOL8_CBSG"]
+           "SC_UNIPOLAR_AND_SM", "SC_RNG_LFSR32", "SC_RNG_SOBOL8_CBSG",
+           "fp8_quantize", "fp8_gemm", "residual_norm", "residual_norm_backward", "rope", "rope_quantize", "rope_table",
+           "SC_BLOCK_1X128", "SC_BLOCK_128X128", "SC_BLOCK_128X1_T", "SC_NORM_NONE", "SC_NORM_RMS", "SC_NORM_LAYER"]
+
+from .layers import (SC_BLOCK_1X128, SC_BLOCK_128X1_T, SC_BLOCK_128X128, SC_NORM_LAYER, SC_NORM_NONE,  # noqa: E402,F401
+                     SC_NORM_RMS, fp8_gemm, fp8_quantize, residual_norm, residual_norm_backward, rope, rope_quantize, rope_table)
 
 
 def _stream_handle(stream, device_index=None):

@@ -12,7 +12,8 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["sc_kernels.hip", "sc_mfma.hip", "sc_frontend.hip", "sc_api.hip"]
+SOURCES = ["sc_kernels.hip", "sc_mfma.hip", "sc_frontend.hip", "sc_fp8.hip", "sc_norm.hip", "sc_rope.hip",
+           "sc_api.hip"]
 OUT = os.path.join(HERE, "libscgemm.so")
 PEAK_SOURCES = ["sc_peak.hip"]
 PEAK_OUT = os.path.join(HERE, "libscpeak.so")

@@ -704,7 +704,7 @@ using namespace scg;
 
 extern "C" {
 
-int sc_version(void) { return 10200; }
+int sc_version(void) { return 10300; }
 
 const char *sc_strerror(int code) {
     switch (code) {
@@ -721,6 +721,7 @@ const char *sc_strerror(int code) {
         case SC_ERR_DEVICE_STATUS: return "SC_ERR_DEVICE_STATUS: some L_i outside [0, L_max]";
         case SC_ERR_STRIDE: return "SC_ERR_STRIDE: a stride is too small or negative";
         case SC_ERR_RESERVED: return "SC_ERR_RESERVED: the reserved descriptor field is not 0";
+        case SC_ERR_TYPE: return "SC_ERR_TYPE: an element type, block, norm or pairing is unknown or not served here";
         default: return "unknown status code";
     }
 }

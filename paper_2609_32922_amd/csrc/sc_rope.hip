@@ -1,0 +1,192 @@
+// Rotary positions with several axes.
+#include <math.h>
+
+#include "sc_layer.h"
+
+namespace scl {
+
+struct RopeArgs {
+    sc_rope_desc d;
+    const void *x;
+    const int32_t *pos;
+    const double *freq;
+    const int32_t *axis;
+    void *out;
+    float *scale, *rowmax;
+    int groups;              // threads of a head's row: each has four pairs, or eight elements that pass
+    int turning;             // of these, those with pairs
+    int heads_each;          // heads that a thread takes one after the other
+    int hblocks;             // groups of heads
+};
+
+// cosine and sine of four pairs of a token.  The turn n = pos freq / 2 pi is formed as an unevaluated sum of two float64
+// (1 / 2 pi is one, and so is its product with freq), so that cutting it to [-1/2, 1/2] loses nothing at any position.
+__device__ __forceinline__ void turns(const RopeArgs &a, int b, int64_t token, int p0, f4 &c, f4 &s) {
+    constexpr double INV_HI = 0x1.45f306dc9c883p-3, INV_LO = -0x1.6b01ec5417056p-57;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int p = p0 + j;
+        double n = 0.0;
+        if (p < a.d.pairs) {
+            const int ax = a.axis[p];
+            if ((unsigned)ax < (unsigned)a.d.axes) {
+                const double f = a.freq[p], pos = (double)a.pos[(int64_t)b * a.d.stridePB + (int64_t)ax * a.d.stridePA + token];
+                const double step = f * INV_HI, rest = fma(f, INV_HI, -step) + f * INV_LO;
+                const double whole = pos * step;
+                n = (whole - rint(whole)) + (fma(pos, step, -whole) + pos * rest);
+            }
+        }
+        float si, co;
+        sincospif((float)(2.0 * n), &si, &co);
+        c[j] = co;
+        s[j] = a.d.inverse ? -si : si;
+    }
+}
+
+// A thread has four pairs of a token (or eight elements that pass) and takes them through heads_each heads with one
+// set of cosines.  Memory-bound.  VEC: rows, pairs and halves on four elements.
+template <bool VEC, bool NEAR>
+__global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int G) {
+    const sc_rope_desc &d = a.d;
+    if (block_id() >= blocks) return;
+    const int sub = threadIdx.x % G;
+    const int64_t unit = (int64_t)block_id() * (256 / G) + threadIdx.x / G;
+    const int64_t token = unit / a.hblocks;
+    const int h0 = (int)(unit % a.hblocks) * a.heads_each, h1 = min(h0 + a.heads_each, d.heads);
+    const bool live = token < d.tokens && sub < a.groups;
+    const int P = d.pairs, p0 = 4 * sub, tail = 2 * P + 8 * (sub - a.turning);
+    // the two quads of a thread: where they start and how many elements they have
+    const bool turn = sub < a.turning;
+    const int e0 = !turn ? tail : NEAR ? 2 * p0 : p0, e1 = !turn ? tail + 4 : NEAR ? 2 * p0 + 4 : P + p0;
+    const int n0 = !live ? 0 : !turn ? min(d.D - e0, 4) : NEAR ? min(2 * P - e0, 4) : min(P - p0, 4);
+    const int n1 = !live ? 0 : !turn ? min(d.D - e1, 4) : NEAR ? min(2 * P - e1, 4) : min(P - p0, 4);
+    for (int b = blockIdx.z; b < d.batch; b += gridDim.z) {
+        f4 c = {1.0f, 1.0f, 1.0f, 1.0f}, s = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (live && turn) turns(a, b, token, p0, c, s);
+        for (int h = h0; h < h1; ++h) {
+            const int64_t at = (int64_t)b * d.strideXB + token * d.strideXT + (int64_t)h * d.strideXH;
+            f4 u = to_floats(d.typeX, load_raw<VEC>(d.typeX, a.x, at + e0, n0));
+            f4 v = to_floats(d.typeX, load_raw<VEC>(d.typeX, a.x, at + e1, n1));
+            f4 o0 = u, o1 = v;
+            if (turn) {
+                if (NEAR) {
+                    o0 = f4{u[0] * c[0] - u[1] * s[0], u[0] * s[0] + u[1] * c[0], u[2] * c[1] - u[3] * s[1], u[2] * s[1] + u[3] * c[1]};
+                    o1 = f4{v[0] * c[2] - v[1] * s[2], v[0] * s[2] + v[1] * c[2], v[2] * c[3] - v[3] * s[3], v[2] * s[3] + v[3] * c[3]};
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        o0[j] = u[j] * c[j] - v[j] * s[j];
+                        o1[j] = u[j] * s[j] + v[j] * c[j];
+                    }
+                }
+            }
+            const int64_t to = (int64_t)b * d.strideOB + token * d.strideOT + (int64_t)h * d.strideOH;
+            if (d.typeO == SC_INT8) {
+                float m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j < n0) m = fmaxf(m, fabsf(o0[j]));
+                    if (j < n1) m = fmaxf(m, fabsf(o1[j]));
+                }
+                for (int o = G / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+                const float sc = m / 127.0f;
+                if (live && sub == 0) {
+                    const int64_t si = (int64_t)b * d.strideSB + token * d.strideST + (int64_t)h * d.strideSH;
+                    a.scale[si] = sc;
+                    if (a.rowmax) a.rowmax[si] = m;
+                }
+                store_bytes4<VEC>(a.out, to + e0, quant_int8x4(o0, sc), n0);
+                store_bytes4<VEC>(a.out, to + e1, quant_int8x4(o1, sc), n1);
+            } else {
+                store4<VEC>(d.typeO, a.out, to + e0, o0, n0);
+                store4<VEC>(d.typeO, a.out, to + e1, o1, n1);
+            }
+        }
+    }
+}
+
+// Whether no two of the n_i elements at strides s_i coincide, as a sufficient test: taken by growing stride, each
+// stride passes what the smaller ones span
+static bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t unit) {
+    int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (s[j] < s[i]) {
+                const int64_t tn = n[i], ts = s[i];
+                n[i] = n[j];
+                s[i] = s[j];
+                n[j] = tn;
+                s[j] = ts;
+            }
+    int64_t span = unit;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] <= 1) continue;
+        if (s[i] < span) return false;
+        span += (n[i] - 1) * s[i];
+    }
+    return true;
+}
+
+}  // namespace scl
+
+using namespace scl;
+
+extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *pos, const double *freq, const int32_t *axis,
+                       void *out, float *scale, float *rowmax, void *stream) {
+    if (desc == nullptr) return SC_ERR_NULL;
+    const sc_rope_desc &d = *desc;
+    if (d.reserved[0] != 0 || d.reserved[1] != 0) return SC_ERR_RESERVED;
+    if (d.batch < 0 || d.tokens < 0 || d.heads < 0 || d.D < 0 || d.D > SC_ROPE_D_LIMIT || d.pairs < 0 || 2 * (int64_t)d.pairs > d.D ||
+        d.axes < 1 || d.axes > SC_ROPE_AXES_LIMIT)
+        return SC_ERR_SHAPE;
+    if (!is_float_type(d.typeX) || (!is_float_type(d.typeO) && d.typeO != SC_INT8)) return SC_ERR_TYPE;
+    if ((d.pairing != SC_ROPE_HALVES && d.pairing != SC_ROPE_NEIGHBOURS) || (d.inverse != 0 && d.inverse != 1)) return SC_ERR_TYPE;
+    const int64_t strides[] = {d.strideXB, d.strideXT, d.strideXH, d.strideOB, d.strideOT, d.strideOH,
+                               d.strideSB, d.strideST, d.strideSH, d.stridePB, d.stridePA};
+    for (int64_t s : strides)
+        if (s < 0) return SC_ERR_STRIDE;
+    if (d.batch == 0 || d.tokens == 0 || d.heads == 0 || (d.D == 0 && d.typeO != SC_INT8)) return SC_OK;
+    if (!apart(d.batch, d.strideOB, d.tokens, d.strideOT, d.heads, d.strideOH, d.D)) return SC_ERR_STRIDE;
+    if (d.typeO == SC_INT8 && !apart(d.batch, d.strideSB, d.tokens, d.strideST, d.heads, d.strideSH, 1)) return SC_ERR_STRIDE;
+    if (d.D > 0 && (x == nullptr || out == nullptr)) return SC_ERR_NULL;
+    if (d.pairs > 0 && (pos == nullptr || freq == nullptr || axis == nullptr)) return SC_ERR_NULL;
+    if (d.typeO == SC_INT8 && scale == nullptr) return SC_ERR_NULL;
+    if (d.typeO != SC_INT8 && rowmax != nullptr) return SC_ERR_TYPE;
+    if (!aligned_to(x, type_bytes(d.typeX)) || !aligned_to(out, type_bytes(d.typeO)) || !aligned_to(pos, 4) || !aligned_to(freq, 8) ||
+        !aligned_to(axis, 4) || !aligned_to(scale, 4) || !aligned_to(rowmax, 4))
+        return SC_ERR_STRIDE;
+    RopeArgs a{};
+    a.d = d;
+    a.x = x;
+    a.pos = pos;
+    a.freq = freq;
+    a.axis = axis;
+    a.out = out;
+    a.scale = scale;
+    a.rowmax = rowmax;
+    a.turning = (d.pairs + 3) / 4;
+    a.groups = a.turning + (d.D - 2 * d.pairs + 7) / 8;
+    if (a.groups < 1) a.groups = 1;
+    // (at most 33 groups, so a head's row lies in one wave, whose lanes take an int8 row's maximum)
+    int G = 1;
+    while (G < a.groups) G <<= 1;
+    a.heads_each = 4;
+    a.hblocks = (d.heads + a.heads_each - 1) / a.heads_each;
+    const int64_t units = (int64_t)d.tokens * a.hblocks, blocks = (units + 256 / G - 1) / (256 / G);
+    if (blocks > INT32_MAX) return SC_ERR_SHAPE;
+    const int64_t xb = 4 * type_bytes(d.typeX), ob = 4 * type_bytes(d.typeO);
+    const bool vec = d.D % 4 == 0 && d.pairs % 4 == 0 && aligned_to(x, xb) && aligned_to(out, ob) &&
+                     d.strideXB % 4 == 0 && d.strideXT % 4 == 0 && d.strideXH % 4 == 0 && d.strideOB % 4 == 0 &&
+                     d.strideOT % 4 == 0 && d.strideOH % 4 == 0;
+    const dim3 grid = grid_of((uint32_t)blocks, d.batch);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const bool near = d.pairing == SC_ROPE_NEIGHBOURS;
+    if (vec) {
+        if (near) hipLaunchKernelGGL((k_rope<true, true>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
+        else hipLaunchKernelGGL((k_rope<true, false>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
+    } else {
+        if (near) hipLaunchKernelGGL((k_rope<false, true>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
+        else hipLaunchKernelGGL((k_rope<false, false>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
+    }
+    return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP;
+}
