@@ -93,18 +93,35 @@ __device__ __forceinline__ void store4(int type, void *p, int64_t at, f4 v, int 
     }
 }
 
-// over groups of W neighbouring lanes (W a power of two), every lane gets the result
-template <int W>
-__device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+// Over groups of W neighbouring lanes (W a power of two), every lane gets the result.  Within 16 lanes by the
+// vector unit's own lane moves, beyond by the swaps of rows and halves: no trip through LDS.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int W, typename F>
+__device__ __forceinline__ float lanes(float v, F f) {
+    if (W >= 2) v = f(v, moved<0xb1>(v));       // quad_perm 1 0 3 2
+    if (W >= 4) v = f(v, moved<0x4e>(v));       // quad_perm 2 3 0 1
+    if (W >= 8) v = f(v, moved<0x141>(v));      // row_half_mirror
+    if (W >= 16) v = f(v, moved<0x140>(v));     // row_mirror
+    if (W >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    if (W >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
     return v;
 }
 template <int W>
+__device__ __forceinline__ float lanes_max(float v) {
+    return lanes<W>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int W>
 __device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    return lanes<W>(v, [](float a, float b) { return a + b; });
 }
 
 // Scale of an fp8 block with largest magnitude m, and its reciprocal.  The scale is at least the least

@@ -18,82 +18,118 @@ struct NormArgs {
     void *dx, *dy;
     float *dpost_w, *dpost_b, *dgate, *dpre_w, *dpre_b;
     float *part;                 // [batch][chunks][NPART][D] partial sums
-    int chunks, chunk_rows;
+    int chunks;
 };
 
-// Sums of N values over a row, which W waves share; every thread gets them
+// A block's threads: RPB rows side by side, W waves each
+template <int W>
+struct Waves {
+    static constexpr int RPB = W >= 8 ? 1 : 8 / W, THREADS = W >= 8 ? 64 * W : 512;
+};
+
+// Sums of N values over a row; every thread of the row gets them.  Rows of several waves meet in LDS, in one of two places
+// by turns, so that one barrier is enough.
 template <int W, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float *lds) {
+struct RowSums {
+    static constexpr int SLOT = N * Waves<W>::RPB * W;
+    float *lds;
+    int turn = 0;
+    __device__ __forceinline__ void operator()(float (&v)[N], int n) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = lanes_sum<64>(v[k]);
-    if (W > 1) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0)
+        for (int k = 0; k < N; ++k)
+            if (k < n) v[k] = lanes_sum<64>(v[k]);
+        if (W > 1) {
+            const int wave = threadIdx.x >> 6, first = wave / W * W;
+            float *s = lds + turn * SLOT;
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) lds[k * W + wave] = v[k];
-        __syncthreads();
+                for (int k = 0; k < N; ++k)
+                    if (k < n) s[wave * N + k] = v[k];
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            v[k] = 0.0f;
-            for (int w = 0; w < W; ++w) v[k] += lds[k * W + w];
+            for (int k = 0; k < N; ++k) {
+                if (k >= n) continue;
+                v[k] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) v[k] += s[(first + w) * N + k];
+            }
         }
     }
-}
-template <int W>
-__device__ __forceinline__ float row_max(float v, float *lds) {
-    v = lanes_max<64>(v);
-    if (W > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        for (int w = 0; w < W; ++w) v = fmaxf(v, lds[w]);
-    }
-    return v;
-}
-
-// A row of D elements by W waves, NV quads a thread: element 4 (64 W k + t) + j is thread t's
-template <int W, int NV>
-struct Row {
-    f4 v[NV];
 };
-template <int W, int NV, bool VEC>
-__device__ __forceinline__ void load_row(Raw4 (&r)[NV], int type, const void *p, int64_t at, int t, int D) {
-    if (type == SC_F32) {
+
+// A row's elements as they lie in memory, NV quads a thread: quad k of thread t is elements 4 (64 W k + t) .. + 3.  R: words of
+// a quad, 2 where the type has 16 bits, 4 where it may be any.
+template <int W, int NV, int R, bool VEC>
+struct RawRow {
+    uint32_t w[NV][R];
+    __device__ __forceinline__ void load(int type, const void *p, int64_t at, int t, int D) {
+        if (R == 4 && type == SC_F32) {
+            const uint32_t *q = static_cast<const uint32_t *>(p) + at;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) r[k] = load_raw<VEC>(SC_F32, p, at + 4 * (64 * W * k + t), D - 4 * (64 * W * k + t));
-    } else {
+            for (int k = 0; k < NV; ++k) {
+                const int d = 4 * (64 * W * k + t);
+                if (VEC) {
+                    u4 x = {0u, 0u, 0u, 0u};
+                    if (d < D) x = *reinterpret_cast<const u4 *>(q + d);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) r[k] = load_raw<VEC>(SC_BF16, p, at + 4 * (64 * W * k + t), D - 4 * (64 * W * k + t));
+                    for (int j = 0; j < R; ++j) w[k][j] = x[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < R; ++j) w[k][j] = d + j < D ? q[d + j] : 0u;
+                }
+            }
+        } else {
+            const uint16_t *q = static_cast<const uint16_t *>(p) + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int d = 4 * (64 * W * k + t);
+                if (VEC) {
+                    u2 x = {0u, 0u};
+                    if (d < D) x = *reinterpret_cast<const u2 *>(q + d);
+                    w[k][0] = x[0];
+                    w[k][1] = x[1];
+                } else {
+                    w[k][0] = w[k][1] = 0u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (d + j < D) w[k][j >> 1] |= (uint32_t)q[d + j] << (16 * (j & 1));
+                }
+            }
+        }
     }
-}
-template <int NV>
-__device__ __forceinline__ void widen(f4 (&v)[NV], int type, const Raw4 (&r)[NV]) {
-    if (type == SC_F32) {
+    __device__ __forceinline__ void widen(int type, f4 (&v)[NV]) const {
+        if (R == 4 && type == SC_F32) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = to_floats(SC_F32, r[k]);
-    } else if (type == SC_BF16) {
+            for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = to_floats(SC_BF16, r[k]);
-    } else {
+                for (int j = 0; j < 4; ++j) v[k][j] = __uint_as_float(w[k][j < R ? j : 0]);
+        } else if (type == SC_BF16) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = to_floats(SC_F16, r[k]);
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][j] = __uint_as_float(j & 1 ? w[k][j >> 1] & 0xffff0000u : w[k][j >> 1] << 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][j] = from_f16((w[k][j >> 1] >> (16 * (j & 1))) & 0xffffu);
+        }
     }
-}
-template <int W, int NV, bool VEC>
+};
+// a parameter's row plus `off`, or `none` where there is no parameter
+template <int W, int NV, int R, bool VEC>
 __device__ __forceinline__ void load_param(f4 (&v)[NV], int type, const void *p, int64_t at, int t, int D, float off, float none) {
     if (p == nullptr) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) v[k] = f4{none, none, none, none};
         return;
     }
-    Raw4 r[NV];
-    load_row<W, NV, VEC>(r, type, p, at, t, D);
-    widen(v, type, r);
+    RawRow<W, NV, R, VEC> r;
+    r.load(type, p, at, t, D);
+    r.widen(type, v);
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] += off;
+    for (int k = 0; k < NV; ++k) v[k] += off;
 }
 template <int W, int NV, bool VEC>
 __device__ __forceinline__ void store_row(int type, void *p, int64_t at, int t, int D, const f4 (&v)[NV]) {
@@ -108,84 +144,94 @@ __device__ __forceinline__ void store_row(int type, void *p, int64_t at, int t, 
         for (int k = 0; k < NV; ++k) store4<VEC>(SC_F16, p, at + 4 * (64 * W * k + t), v[k], D - 4 * (64 * W * k + t));
     }
 }
-
-// v normalised in place (elements past D become 0); returns 1 / deviation.  The mean is taken before the squares,
-// which therefore lose nothing to it.
+template <int NV>
+__device__ __forceinline__ float sum(const f4 (&v)[NV]) {
+    f4 s = v[0];
+#pragma unroll
+    for (int k = 1; k < NV; ++k) s += v[k];
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+template <int NV>
+__device__ __forceinline__ float dot(const f4 (&u)[NV], const f4 (&v)[NV]) {
+    f4 s = u[0] * v[0];
+#pragma unroll
+    for (int k = 1; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = fmaf(u[k][j], v[k][j], s[j]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+// v - m where there are elements, 0 behind them
 template <int W, int NV>
-__device__ __forceinline__ float normalise(f4 (&v)[NV], int kind, float eps, int t, int D, float *lds) {
-    if (kind == SC_NORM_LAYER) {
-        float s[1] = {0.0f};
-#pragma unroll
-        for (int k = 0; k < NV; ++k) s[0] += (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
-        row_sums<W, 1>(s, lds);
-        const float mean = s[0] / (float)D;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[k][j] = 4 * (64 * W * k + t) + j < D ? v[k][j] - mean : 0.0f;
-    }
-    float q[1] = {0.0f};
-#pragma unroll
-    for (int k = 0; k < NV; ++k) q[0] += (v[k][0] * v[k][0] + v[k][1] * v[k][1]) + (v[k][2] * v[k][2] + v[k][3] * v[k][3]);
-    row_sums<W, 1>(q, lds);
-    const float r = 1.0f / sqrtf(q[0] / (float)D + eps);
+__device__ __forceinline__ void centre(f4 (&v)[NV], float m, int t, int D) {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] *= r;
-    return r;
+        for (int j = 0; j < 4; ++j) v[k][j] = 4 * (64 * W * k + t) + j < D ? v[k][j] - m : 0.0f;
+}
+// 1 / sqrt(mean + eps), to a rounding of each step
+__device__ __forceinline__ float inverse_deviation(float squares, float n, float eps) { return 1.0f / sqrtf(squares / n + eps); }
+
+// v normalised in place (elements past D become 0).  The mean is taken before the squares, which therefore lose
+// nothing to it.
+template <int W, int NV, typename Sums>
+__device__ __forceinline__ void normalise(f4 (&v)[NV], int kind, float eps, int t, int D, Sums &sums) {
+    if (kind == SC_NORM_LAYER) {
+        float s[1] = {sum(v)};
+        sums(s, 1);
+        centre<W>(v, s[0] / (float)D, t, D);
+    }
+    float q[1] = {dot(v, v)};
+    sums(q, 1);
+    const float r = inverse_deviation(q[0], (float)D, eps);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) v[k] *= r;
 }
 
 // One row by W waves, held in registers from its loads to its stores: every operand is read once and every
 // result written once.  Memory-bound.
-template <int W, int NV, bool VEC>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
-    constexpr int RPB = W == 1 ? 4 : 1;           // rows of a block
-    __shared__ float lds[W];
-    const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t i = (int64_t)block_id() * RPB + (W == 1 ? threadIdx.x >> 6 : 0);
-    if (i >= a.rows) return;
-    const int D = a.D;
+template <int W, int NV, int RX, int RY, bool VEC>
+__global__ __launch_bounds__(Waves<W>::THREADS) void k_norm(NormArgs a) {
+    constexpr int RPB = Waves<W>::RPB;
+    __shared__ float lds[2 * RPB * W];
+    RowSums<W, 1> sums{lds};
+    const int t = threadIdx.x % (64 * W), D = a.D;
+    const int64_t row = (int64_t)block_id() * RPB + threadIdx.x / (64 * W);
+    const bool live = row < a.rows;
+    if (W == 1 && !live) return;          // (rows of several waves meet at barriers, so all of a block's stay)
+    const int64_t i = min(row, (int64_t)a.rows - 1);
     for (int b = blockIdx.z; b < a.batch; b += gridDim.z) {
-        Raw4 rx[NV], ry[NV];
-        load_row<W, NV, VEC>(rx, a.typeX, a.x, (int64_t)b * a.strideX + i * a.ldx, t, D);
-        if (a.y) load_row<W, NV, VEC>(ry, a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
+        RawRow<W, NV, RX, VEC> rx;
+        RawRow<W, NV, RY, VEC> ry;
+        rx.load(a.typeX, a.x, (int64_t)b * a.strideX + i * a.ldx, t, D);
+        if (a.y) ry.load(a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
         f4 x[NV];
-        widen(x, a.typeX, rx);
+        rx.widen(a.typeX, x);
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[k][j] *= a.scale_res;
+        for (int k = 0; k < NV; ++k) x[k] *= a.scale_res;
         if (a.y) {
             f4 u[NV], w[NV];
-            widen(u, a.typeY, ry);
+            ry.widen(a.typeY, u);
             if (a.post != SC_NORM_NONE) {
-                normalise<W, NV>(u, a.post, a.eps_post, t, D, lds);
+                normalise<W>(u, a.post, a.eps_post, t, D, sums);
                 f4 c[NV];
-                load_param<W, NV, VEC>(w, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
-                load_param<W, NV, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
+                load_param<W, NV, RY, VEC>(w, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
+                load_param<W, NV, RY, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) u[k][j] = u[k][j] * w[k][j] + c[k][j];
+                for (int k = 0; k < NV; ++k) u[k] = u[k] * w[k] + c[k];
             }
-            load_param<W, NV, VEC>(w, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
+            load_param<W, NV, RY, VEC>(w, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][j] += u[k][j] * w[k][j];
+            for (int k = 0; k < NV; ++k) x[k] += u[k] * w[k];
         }
-        if (a.xo) store_row<W, NV, VEC>(a.typeX, a.xo, (int64_t)b * a.strideXO + i * a.ldxo, t, D, x);
+        if (a.xo && live) store_row<W, NV, VEC>(a.typeX, a.xo, (int64_t)b * a.strideXO + i * a.ldxo, t, D, x);
         if (a.h == nullptr) continue;
         if (a.pre != SC_NORM_NONE) {
-            normalise<W, NV>(x, a.pre, a.eps_pre, t, D, lds);
+            normalise<W>(x, a.pre, a.eps_pre, t, D, sums);
             f4 w[NV], c[NV];
-            load_param<W, NV, VEC>(w, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
-            load_param<W, NV, VEC>(c, a.typeP, a.pre_b, (int64_t)b * a.s_pre_b, t, D, 0.0f, 0.0f);
+            load_param<W, NV, RY, VEC>(w, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
+            load_param<W, NV, RY, VEC>(c, a.typeP, a.pre_b, (int64_t)b * a.s_pre_b, t, D, 0.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[k][j] = x[k][j] * w[k][j] + c[k][j];
+            for (int k = 0; k < NV; ++k) x[k] = x[k] * w[k] + c[k];
         }
         const int64_t ho = (int64_t)b * a.strideH + i * a.ldh;
         if (a.typeH == SC_INT8) {
@@ -194,7 +240,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) m = 4 * (64 * W * k + t) + j < D ? fmaxf(m, fabsf(x[k][j])) : m;
-            m = row_max<W>(m, lds);
+            m = lanes_max<64>(m);
+            if (W > 1) {
+                __shared__ float most[RPB * W];
+                const int wave = threadIdx.x >> 6, first = wave / W * W;
+                __syncthreads();
+                if ((threadIdx.x & 63) == 0) most[wave] = m;
+                __syncthreads();
+                for (int w = 0; w < W; ++w) m = fmaxf(m, most[first + w]);
+            }
+            if (!live) continue;
             const float s = m / 127.0f;
             if (t == 0) {
                 a.scale[(int64_t)b * a.strideS + i] = s;
@@ -205,6 +260,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
                 store_bytes4<VEC>(a.h, ho + 4 * (64 * W * k + t), quant_int8x4(x[k], s), D - 4 * (64 * W * k + t));
         } else if (a.typeH == SC_E4M3 || a.typeH == SC_E5M2) {
             // a block of 128 is the quads of 32 neighbouring lanes
+            if (!live) continue;
             const bool e5 = a.typeH == SC_E5M2;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -217,7 +273,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
                 if ((t & 31) == 0 && d < D) a.scale[(int64_t)b * a.strideS + i * a.lds + (d >> 7)] = s.s;
                 store_bytes4<VEC>(a.h, ho + d, quant_fp8x4(e5, x[k], s.inv), D - d);
             }
-        } else {
+        } else if (live) {
             store_row<W, NV, VEC>(a.typeH, a.h, ho, t, D, x);
         }
     }
@@ -228,123 +284,132 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a) {
 // ----------------------------------------------------------------------------
 enum { P_PRE_W, P_PRE_B, P_GATE, P_POST_W, P_POST_B, NPART };
 
-// The gradient before a norm, in place of the one behind it (d, already times the weight): with n the normalised
-// row and r = 1 / deviation, r (d - n mean(d n)), LayerNorm also - mean(d)
-template <int W, int NV>
-__device__ __forceinline__ void norm_back(f4 (&d)[NV], const f4 (&n)[NV], float r, int kind, int D, float *lds) {
-    float s[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            s[0] += d[k][j] * n[k][j];
-            s[1] += d[k][j];
-        }
-    row_sums<W, 2>(s, lds);
-    const float dn = s[0] / (float)D, dm = kind == SC_NORM_LAYER ? s[1] / (float)D : 0.0f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[k][j] = r * (d[k][j] - dm - n[k][j] * dn);
-}
-
-template <int NV>
-__device__ __forceinline__ void zero(f4 (&v)[NV]) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-}
-
-// A block takes chunk_rows rows of a batch entry, RPB at a time, and sums its rows' shares of the parameters'
-// gradients in registers; the blocks' sums go to memory and k_norm_sums adds them in a fixed order.  POST: a norm
-// behind the branch.
-template <int W, int NV, bool VEC, bool POST>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a) {
-    constexpr int RPB = W == 1 ? 4 : 1, NP = POST ? 5 : 3;
-    __shared__ float lds[2 * W];
-    __shared__ f4 join[W == 1 ? 3 * 64 : 1];
-    const int t = W == 1 ? threadIdx.x & 63 : threadIdx.x, grp = W == 1 ? threadIdx.x >> 6 : 0;
+// A block takes a run of a batch entry's rows, RPB side by side, and sums its rows' shares of the parameters' gradients in
+// registers; the blocks' sums go to memory and k_norm_sums adds them in a fixed order.  The next row is loaded while one is
+// worked on.  With n the normalised row, r = 1 / deviation and d the gradient behind the norm times its weight, the
+// gradient before it is r (d - n mean(d n)), LayerNorm also - mean(d); both means and the deviation come from one round of
+// sums.  POST: a norm behind the branch.  Memory-bound.
+template <int W, int NV, int RX, int RY, bool VEC, bool POST>
+__global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back(NormArgs a) {
+    constexpr int RPB = Waves<W>::RPB, NP = POST ? 5 : 3, NS = 4;
+    __shared__ float lds[2 * NS * RPB * W];
+    __shared__ f4 join[RPB > 1 ? (RPB - 1) * 64 * W : 1];
+    RowSums<W, NS> sums{lds};
+    const int t = threadIdx.x % (64 * W), side = threadIdx.x / (64 * W), D = a.D;
     const int64_t chunk = block_id();
     if (chunk >= a.chunks) return;
-    const int D = a.D;
-    const int64_t i1 = min((chunk + 1) * a.chunk_rows, (int64_t)a.rows);
+    const int64_t i0 = chunk * a.rows / a.chunks, i1 = (chunk + 1) * a.rows / a.chunks;
+    const float n_inv = 1.0f / (float)D;
     for (int b = blockIdx.z; b < a.batch; b += gridDim.z) {
-        f4 sum[NP][NV];
+        f4 acc[NP][NV];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) zero(sum[p]);
-        for (int64_t i = chunk * a.chunk_rows + grp; i < i1; i += RPB) {
-            Raw4 rx[NV], ry[NV], rg[NV], rh[NV];
-            if (a.x) load_row<W, NV, VEC>(rx, a.typeX, a.x, (int64_t)b * a.strideXO + i * a.ldxo, t, D);
-            if (a.y) load_row<W, NV, VEC>(ry, a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
-            if (a.dxo) load_row<W, NV, VEC>(rg, a.typeX, a.dxo, (int64_t)b * a.strideDXO + i * a.lddxo, t, D);
-            if (a.dh) load_row<W, NV, VEC>(rh, a.typeH, a.dh, (int64_t)b * a.strideH + i * a.ldh, t, D);
-            f4 g[NV];
-            if (a.dh) {
-                f4 n[NV], w[NV];
-                widen(g, a.typeH, rh);
-                if (a.pre != SC_NORM_NONE) {
-                    widen(n, a.typeX, rx);
-                    const float r = normalise<W, NV>(n, a.pre, a.eps_pre, t, D, lds);
-                    load_param<W, NV, VEC>(w, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) acc[p][k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        RawRow<W, NV, RX, VEC> rx, rg;
+        RawRow<W, NV, RY, VEC> ry, rh;
+        const auto fetch = [&](int64_t row) {
+            const int64_t i = min(row, i1 - 1);
+            if (a.x) rx.load(a.typeX, a.x, (int64_t)b * a.strideXO + i * a.ldxo, t, D);
+            if (a.dh) rh.load(a.typeH, a.dh, (int64_t)b * a.strideH + i * a.ldh, t, D);
+            if (a.y) ry.load(a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
+            if (a.dxo) rg.load(a.typeX, a.dxo, (int64_t)b * a.strideDXO + i * a.lddxo, t, D);
+        };
+        fetch(i0 + side);
+        for (int64_t first = i0; first < i1; first += RPB) {
+            const int64_t i = first + side;
+            const bool live = i < i1;               // (a row behind the last takes part in barriers and counts nothing)
+            if (W == 1 && !live) break;
+            f4 n[NV], g[NV], e[NV], m[NV];
+            if (a.x) rx.widen(a.typeX, n);
+            if (a.dh) rh.widen(a.typeH, g);
+            if (a.y) ry.widen(a.typeY, m);
+            if (a.dxo) rg.widen(a.typeX, e);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (!a.dh || !live) g[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (!a.dxo || !live) e[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (!a.y) m[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            fetch(i + RPB);
+            const bool pre = a.pre != SC_NORM_NONE && a.dh, pre_mean = pre && a.pre == SC_NORM_LAYER,
+                       post_mean = POST && a.post == SC_NORM_LAYER;
+            if (pre_mean || post_mean) {
+                float s[NS] = {pre ? sum(n) : 0.0f, POST ? sum(m) : 0.0f, 0.0f, 0.0f};
+                sums(s, 2);
+                if (pre_mean) centre<W>(n, s[0] * n_inv, t, D);
+                if (post_mean) centre<W>(m, s[1] * n_inv, t, D);
+            }
+            float r_post = 1.0f;
+            if (pre || POST) {
+                f4 d[NV];
+                float s[NS] = {0.0f, 0.0f, 0.0f, POST ? dot(m, m) : 0.0f};
+                if (pre) {
+                    load_param<W, NV, RY, VEC>(d, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) d[k] *= g[k];
+                    s[0] = dot(n, n);
+                    s[1] = dot(d, n);
+                    s[2] = sum(d);
+                }
+                sums(s, NS);
+                if (POST) r_post = inverse_deviation(s[3], (float)D, a.eps_post);
+                if (pre) {
+                    const float r = inverse_deviation(s[0], (float)D, a.eps_pre), dn = s[1] * r * n_inv,
+                                dm = pre_mean ? s[2] * n_inv : 0.0f;
 #pragma unroll
                     for (int k = 0; k < NV; ++k)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            sum[P_PRE_W][k][j] += g[k][j] * n[k][j];
-                            sum[P_PRE_B][k][j] += g[k][j];
-                            g[k][j] *= w[k][j];
+                            const float nr = n[k][j] * r;
+                            acc[P_PRE_W][k][j] = fmaf(g[k][j], nr, acc[P_PRE_W][k][j]);
+                            acc[P_PRE_B][k][j] += g[k][j];
+                            g[k][j] = fmaf(r, d[k][j] - dm - nr * dn, e[k][j]);
                         }
-                    norm_back<W, NV>(g, n, r, a.pre, D, lds);
                 }
-            } else {
-                zero(g);
             }
-            if (a.dxo) {
-                f4 e[NV];
-                widen(e, a.typeX, rg);
+            if (!pre)
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+                for (int k = 0; k < NV; ++k) g[k] += e[k];
+            if (a.dx && live) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) g[k][j] += e[k][j];
-            }
-            if (a.dx) {
-                f4 e[NV];
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) e[k][j] = a.scale_res * g[k][j];
+                for (int k = 0; k < NV; ++k) e[k] = a.scale_res * g[k];
                 store_row<W, NV, VEC>(a.typeX, a.dx, (int64_t)b * a.strideX + i * a.ldx, t, D, e);
             }
             if (a.y == nullptr && a.dy == nullptr) continue;
-            f4 w[NV], n[NV];
-            load_param<W, NV, VEC>(w, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
-            if (a.y) widen(n, a.typeY, ry);
-            else zero(n);
+            load_param<W, NV, RY, VEC>(e, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
             if (POST) {
                 f4 pw[NV], c[NV];
-                const float r = normalise<W, NV>(n, a.post, a.eps_post, t, D, lds);
-                load_param<W, NV, VEC>(pw, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
-                load_param<W, NV, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
+                load_param<W, NV, RY, VEC>(pw, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
+                load_param<W, NV, RY, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        sum[P_GATE][k][j] += g[k][j] * (n[k][j] * pw[k][j] + c[k][j]);
-                        const float du = g[k][j] * w[k][j];
-                        sum[NP - 2][k][j] += du * n[k][j];
-                        sum[NP - 1][k][j] += du;
+                        const float nr = m[k][j] * r_post, du = g[k][j] * e[k][j];
+                        m[k][j] = nr;
+                        acc[P_GATE][k][j] = fmaf(g[k][j], fmaf(nr, pw[k][j], c[k][j]), acc[P_GATE][k][j]);
+                        acc[NP - 2][k][j] = fmaf(du, nr, acc[NP - 2][k][j]);
+                        acc[NP - 1][k][j] += du;
                         g[k][j] = du * pw[k][j];
                     }
-                if (a.dy) norm_back<W, NV>(g, n, r, a.post, D, lds);
+                if (a.dy) {
+                    float s[NS] = {dot(g, m), sum(g), 0.0f, 0.0f};
+                    sums(s, 2);
+                    const float dn = s[0] * n_inv, dm = post_mean ? s[1] * n_inv : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) g[k] = r_post * (g[k] - dm - m[k] * dn);
+                }
             } else {
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        sum[P_GATE][k][j] += g[k][j] * n[k][j];
-                        g[k][j] *= w[k][j];
+                        acc[P_GATE][k][j] = fmaf(g[k][j], m[k][j], acc[P_GATE][k][j]);
+                        g[k][j] *= e[k][j];
                     }
             }
-            if (a.dy) store_row<W, NV, VEC>(a.typeY, a.dy, (int64_t)b * a.strideDY + i * a.lddy, t, D, g);
+            if (a.dy && live) store_row<W, NV, VEC>(a.typeY, a.dy, (int64_t)b * a.strideDY + i * a.lddy, t, D, g);
         }
         if (a.part == nullptr) continue;
         float *part = a.part + ((int64_t)b * a.chunks + chunk) * NPART * D;
@@ -355,18 +420,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a)
             if (!wanted) continue;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (W == 1) {
+                if (RPB > 1) {
                     __syncthreads();
-                    if (grp > 0) join[(grp - 1) * 64 + t] = sum[p][k];
+                    if (side > 0) join[(side - 1) * 64 * W + t] = acc[p][k];
                     __syncthreads();
-                    if (grp > 0) continue;
+                    if (side > 0) continue;
 #pragma unroll
-                    for (int o = 0; o < 3; ++o)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) sum[p][k][j] += join[o * 64 + t][j];
+                    for (int o = 0; o < RPB - 1; ++o) acc[p][k] += join[o * 64 * W + t];
                 }
                 const int d = 4 * (64 * W * k + t);
-                store4<VEC>(SC_F32, part, (int64_t)p * D + d, sum[p][k], D - d);
+                store4<VEC>(SC_F32, part, (int64_t)p * D + d, acc[p][k], D - d);
             }
         }
     }
@@ -385,6 +448,7 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a) {
         const float *q = a.part + ((int64_t)b * a.chunks * NPART + p) * a.D + d;
         float s = 0.0f;
         if (d < a.D)
+#pragma unroll 8
             for (int64_t k = grp; k < n; k += 16) s += q[k * NPART * a.D];
         __syncthreads();
         join[grp][c] = s;
@@ -400,47 +464,68 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a) {
 // ----------------------------------------------------------------------------
 // host
 // ----------------------------------------------------------------------------
-template <int W, int NV>
-static void launch_norm(const NormArgs &a, bool vec, hipStream_t st) {
-    const dim3 grid = grid_of((uint32_t)(((int64_t)a.rows + (W == 1 ? 3 : 0)) / (W == 1 ? 4 : 1)), a.batch), block(W == 1 ? 256 : 64 * W);
-    constexpr int SCALAR_W = W == 1 ? 1 : 16, SCALAR_NV = W == 1 ? 5 : 4;     // (shape_of without vec)
-    if (vec) hipLaunchKernelGGL((k_norm<W, NV, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_norm<SCALAR_W, SCALAR_NV, false>), grid, block, 0, st, a);
+enum { ANY_ANY, ANY_16, ALL_16 };     // types of the residual stream, and of the rest
+
+template <int W, int NV, int RX, int RY, bool VEC>
+static void launch_forward(const NormArgs &a, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)(((int64_t)a.rows + Waves<W>::RPB - 1) / Waves<W>::RPB);
+    hipLaunchKernelGGL((k_norm<W, NV, RX, RY, VEC>), grid_of(blocks, a.batch), dim3(Waves<W>::THREADS), 0, st, a);
+}
+template <int W, int NV, int RX, int RY, bool VEC>
+static void launch_backward(const NormArgs &a, hipStream_t st) {
+    const dim3 grid = grid_of((uint32_t)a.chunks, a.batch), block(Waves<W>::THREADS);
+    if (a.post != SC_NORM_NONE) hipLaunchKernelGGL((k_norm_back<W, NV, RX, RY, VEC, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_norm_back<W, NV, RX, RY, VEC, false>), grid, block, 0, st, a);
 }
 template <int W, int NV>
-static void launch_back(const NormArgs &a, bool vec, hipStream_t st) {
-    const dim3 grid = grid_of((uint32_t)a.chunks, a.batch), block(W == 1 ? 256 : 64 * W);
-    constexpr int SCALAR_W = W == 1 ? 1 : 16, SCALAR_NV = W == 1 ? 5 : 4;
-    if (a.post != SC_NORM_NONE) {
-        if (vec) hipLaunchKernelGGL((k_norm_back<W, NV, true, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((k_norm_back<SCALAR_W, SCALAR_NV, false, true>), grid, block, 0, st, a);
+static void forward_of(const NormArgs &a, int types, hipStream_t st) {
+    if (types == ALL_16) launch_forward<W, NV, 2, 2, true>(a, st);
+    else if (types == ANY_16) launch_forward<W, NV, 4, 2, true>(a, st);
+    else launch_forward<W, NV, 4, 4, true>(a, st);
+}
+template <int W, int NV>
+static void backward_of(const NormArgs &a, int types, hipStream_t st) {
+    if (types == ALL_16) launch_backward<W, NV, 2, 2, true>(a, st);
+    else if (types == ANY_16) launch_backward<W, NV, 4, 2, true>(a, st);
+    else launch_backward<W, NV, 4, 4, true>(a, st);
+}
+// Forward: the fewest waves that hold a row in five quads a thread (four from 1280 elements on).  Backward: two (three)
+// quads, whose sums leave registers for the next row.  Rows that are read element by element (an odd length or
+// alignment) have two sizes only.
+static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_t st) {
+    const bool x16 = a.typeX != SC_F32, rest16 = (a.y == nullptr || a.typeY != SC_F32) && a.typeP != SC_F32 && (!back || a.dh == nullptr || a.typeH != SC_F32);
+    const int types = x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;
+    if (!vec && back) {
+        if (D <= 512) launch_backward<1, 2, 4, 4, false>(a, st);
+        else if (D <= 4096) launch_backward<8, 2, 4, 4, false>(a, st);
+        else launch_backward<16, 4, 4, 4, false>(a, st);
+    } else if (!vec) {
+        if (D <= 1280) launch_forward<1, 5, 4, 4, false>(a, st);
+        else launch_forward<16, 4, 4, 4, false>(a, st);
+    } else if (back) {
+        if (D <= 512) backward_of<1, 2>(a, types, st);
+        else if (D <= 1024) backward_of<2, 2>(a, types, st);
+        else if (D <= 1536) backward_of<2, 3>(a, types, st);
+        else if (D <= 2048) backward_of<4, 2>(a, types, st);
+        else if (D <= 4096) backward_of<8, 2>(a, types, st);
+        else if (D <= 8192) backward_of<16, 2>(a, types, st);
+        else backward_of<16, 4>(a, types, st);
     } else {
-        if (vec) hipLaunchKernelGGL((k_norm_back<W, NV, true, false>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((k_norm_back<SCALAR_W, SCALAR_NV, false, false>), grid, block, 0, st, a);
+        if (D <= 512) forward_of<1, 2>(a, types, st);
+        else if (D <= 1024) forward_of<1, 4>(a, types, st);
+        else if (D <= 1280) forward_of<1, 5>(a, types, st);
+        else if (D <= 2048) forward_of<2, 4>(a, types, st);
+        else if (D <= 4096) forward_of<4, 4>(a, types, st);
+        else if (D <= 8192) forward_of<8, 4>(a, types, st);
+        else forward_of<16, 4>(a, types, st);
     }
+    return hipGetLastError();
 }
 
-struct Shape {
-    int W, NV;
-};
-// The fewest waves that hold a row in five quads a thread (four from 1280 elements on), and the fewest quads.  Rows
-// that are read element by element (an odd length or alignment) have two sizes only.
-static Shape shape_of(int D, bool vec) {
-    if (!vec) return D <= 1280 ? Shape{1, 5} : Shape{16, 4};
-    if (D <= 1280) return {1, D <= 256 ? 1 : (D + 255) / 256};
-    if (D <= 2048) return {2, 4};
-    if (D <= 4096) return {4, D <= 3 * 1024 ? 3 : 4};
-    return {16, D <= 8192 ? 2 : 4};
-}
-
-// rows of a chunk: about four blocks for each compute unit, and at least four rows in each
-static void chunks_of(const sc_norm_desc &d, int *chunks, int *chunk_rows) {
-    const int64_t want = 1024 / (d.batch > 0 ? d.batch : 1) + 1;
-    int64_t rows = ((int64_t)d.rows + want - 1) / want;
-    rows = (rows + 3) / 4 * 4;
-    if (rows < 4) rows = 4;
-    *chunk_rows = (int)rows;
-    *chunks = (int)(((int64_t)d.rows + rows - 1) / rows);
+// Runs of rows whose sums go to memory: one for each compute unit, which then has eight waves of them
+static int chunks_of(const sc_norm_desc &d) {
+    const int want = d.batch < 1 ? 1 : d.batch < 256 ? (256 + d.batch - 1) / d.batch : 1;
+    return d.rows < want ? d.rows : want;
 }
 
 static int check_norm(const sc_norm_desc *d) {
@@ -516,27 +601,6 @@ static bool params_quads(const sc_norm_desc &d, const void *const (&p)[5]) {
     return true;
 }
 
-#define SCL_BY_SHAPE(LAUNCH, s, ...)                          \
-    do {                                                      \
-        if ((s).W == 1) {                                     \
-            switch ((s).NV) {                                 \
-                case 1: LAUNCH<1, 1>(__VA_ARGS__); break;     \
-                case 2: LAUNCH<1, 2>(__VA_ARGS__); break;     \
-                case 3: LAUNCH<1, 3>(__VA_ARGS__); break;     \
-                case 4: LAUNCH<1, 4>(__VA_ARGS__); break;     \
-                default: LAUNCH<1, 5>(__VA_ARGS__); break;    \
-            }                                                 \
-        } else if ((s).W == 2) {                              \
-            LAUNCH<2, 4>(__VA_ARGS__);                        \
-        } else if ((s).W == 4) {                              \
-            if ((s).NV == 3) LAUNCH<4, 3>(__VA_ARGS__);       \
-            else LAUNCH<4, 4>(__VA_ARGS__);                   \
-        } else {                                              \
-            if ((s).NV == 2) LAUNCH<16, 2>(__VA_ARGS__);      \
-            else LAUNCH<16, 4>(__VA_ARGS__);                  \
-        }                                                     \
-    } while (0)
-
 }  // namespace scl
 
 using namespace scl;
@@ -583,8 +647,7 @@ int sc_residual_norm(const sc_norm_desc *desc, const void *x, const void *y, con
     const bool vec = d.D % 4 == 0 && quads(x, d.typeX, d.ldx, d.strideX) && quads(y, d.typeY, d.ldy, d.strideY) &&
                      quads(xo, d.typeX, d.ldxo, d.strideXO) && quads(h, d.typeH, d.ldh, d.strideH) && params_quads(d, params);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    SCL_BY_SHAPE(launch_norm, shape_of(d.D, vec), a, vec, st);
-    return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP;
+    return launch_rows(a, false, vec, st) == hipSuccess ? SC_OK : SC_ERR_HIP;
 }
 
 int sc_residual_norm_backward_workspace_size(const sc_norm_desc *desc, size_t *bytes) {
@@ -592,9 +655,7 @@ int sc_residual_norm_backward_workspace_size(const sc_norm_desc *desc, size_t *b
     const int rc = check_norm(desc);
     if (rc != SC_OK) return rc;
     if (!is_float_type(desc->typeH)) return SC_ERR_TYPE;
-    int chunks, chunk_rows;
-    chunks_of(*desc, &chunks, &chunk_rows);
-    *bytes = (size_t)desc->batch * chunks * NPART * desc->D * sizeof(float);
+    *bytes = (size_t)desc->batch * chunks_of(*desc) * NPART * desc->D * sizeof(float);
     return SC_OK;
 }
 
@@ -645,15 +706,12 @@ int sc_residual_norm_backward(const sc_norm_desc *desc, const void *xo, const vo
     a.dpre_w = dpre_w;
     a.dpre_b = dpre_b;
     a.part = any ? static_cast<float *>(workspace) : nullptr;
-    chunks_of(d, &a.chunks, &a.chunk_rows);
+    a.chunks = chunks_of(d);
     const bool vec = d.D % 4 == 0 && quads(xo, d.typeX, d.ldxo, d.strideXO) && quads(y, d.typeY, d.ldy, d.strideY) &&
                      quads(dxo, d.typeX, d.lddxo, d.strideDXO) && quads(dh, d.typeH, d.ldh, d.strideH) &&
                      quads(dx, d.typeX, d.ldx, d.strideX) && quads(dy, d.typeY, d.lddy, d.strideDY) && params_quads(d, params);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (rows) {
-        SCL_BY_SHAPE(launch_back, shape_of(d.D, vec), a, vec, st);
-        if (hipGetLastError() != hipSuccess) return SC_ERR_HIP;
-    }
+    if (rows && launch_rows(a, true, vec, st) != hipSuccess) return SC_ERR_HIP;
     // (without rows the sums are zeros)
     if (any) {
         hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((d.D + 63) / 64), NPART, (unsigned)(d.batch < 1 ? 1 : d.batch < 32768 ? d.batch : 32768)),

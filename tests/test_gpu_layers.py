@@ -476,7 +476,9 @@ def test_residual_norm_backward_forms(scg):
     some = scg.residual_norm_backward(xo, y, dxo=dxo, dh=dh, post=1, pre=2, want_params=False, want_x=False, **p)
     assert set(some) == {"y"} and torch.equal(some["y"], full["y"])
     alone = scg.residual_norm_backward(xo, dxo=dxo, dh=dh, pre=2, pre_weight=p["pre_weight"], pre_bias=p["pre_bias"])
-    assert all(torch.equal(alone[k], full[k]) for k in ("x", "pre_weight", "pre_bias"))
+    # (another kernel than the one with a norm behind the branch: the same sums, in roundings of its own)
+    assert set(alone) == {"x", "pre_weight", "pre_bias"}
+    _check_gradients(alone, xo, y, {k: p[k] for k in ("pre_weight", "pre_bias")}, dxo, dh, 0, 2, {})
     none = scg.residual_norm_backward(xo[:, :0], y[:, :0], dxo=dxo[:, :0], dh=dh[:, :0], post=1, pre=2, **p)
     assert all(bool((none[k] == 0).all()) for k in p) and none["x"].shape == (2, 0, 256)
 
