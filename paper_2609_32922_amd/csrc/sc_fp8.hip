@@ -255,7 +255,7 @@ struct GemmArgs {
 template <int T, bool EXACT>
 struct Frag {
     v8i w;
-    __device__ __forceinline__ void set(u4 lo, u4 hi) {
+    __device__ __forceinline__ void set(u4 lo, u4 hi) {      // the granules that a lane holds
         w = v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
     }
 };
@@ -307,10 +307,53 @@ __device__ __forceinline__ void store_out4(const GemmArgs &g, int b, int64_t i, 
 // q ^ swz(r), so that the 16 rows that a fragment read takes at one granule spread over all banks
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 
+// Copies 16 (or 4) bytes for each lane from the buffer, at off, to LDS, at `to` (the same in every lane) plus 16 (4)
+// bytes a lane, past the registers.  Nothing waits for it but wait_copies().  What lies behind the buffer's bound
+// leaves no byte of another row in LDS, and only rows that are not stored have any.
+typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Buffer buffer_of(const void *p, int64_t bytes) {
+    const uint64_t x = (uint64_t)p;
+    return Buffer{(uint32_t)x, (uint32_t)(x >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+}
+__device__ __forceinline__ Buffer advanced(Buffer s, uint32_t bytes) {
+    const uint64_t x = ((uint64_t)s[1] << 32 | s[0]) + bytes;
+    return Buffer{(uint32_t)x, (uint32_t)(x >> 32), s[2] - min(s[2], bytes), s[3]};
+}
+__device__ __forceinline__ Buffer scalar(Buffer s) {      // (it is the same in every lane; told to the compiler)
+    return Buffer{(uint32_t)__builtin_amdgcn_readfirstlane((int)s[0]), (uint32_t)__builtin_amdgcn_readfirstlane((int)s[1]),
+                  (uint32_t)__builtin_amdgcn_readfirstlane((int)s[2]), 0x00020000u};
+}
+__device__ __forceinline__ void copy16(Buffer s, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory");
+}
+__device__ __forceinline__ void copy4(Buffer s, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+
+// a word's bytes before the n-th
+__device__ __forceinline__ uint32_t bytes_before(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
+
+// Where a block's tile starts, in an order that keeps neighbours together on an XCD (blocks are dealt to the eight
+// XCDs in turn, and each has an L2 of its own): a contiguous run of tiles for each, in groups of eight tile rows
+__device__ __forceinline__ void tile_at(uint32_t id, uint32_t tiles, int tilesM, int tilesN, int *b, int *tm, int *tn) {
+    const uint32_t xcd = id & 7u, each = tiles >> 3, more = tiles & 7u;
+    const uint32_t all = xcd * each + (xcd < more ? xcd : more) + (id >> 3), per = (uint32_t)tilesM * (uint32_t)tilesN;
+    const uint32_t entry = all / per, at = all - entry * per;
+    const uint32_t group = at / (8u * (uint32_t)tilesN), in = at - group * 8u * (uint32_t)tilesN;
+    const uint32_t rows = min(8u, (uint32_t)tilesM - 8u * group);
+    *b = (int)entry;
+    *tm = (int)(8u * group + in % rows);
+    *tn = (int)(in / rows);
+}
+
 // A tile of BM x BN outputs by waves of WM x WN each.  A scale block is one stage: the matrix cores sum its
 // 128 products from zero and the sum enters the accumulators times its two scales.
 template <int TA, int TB, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArgs g) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_any(GemmArgs g) {
     constexpr int NT = (BM / WM) * (BN / WN) * 64, MI = WM / 16, NI = WN / 16, GA = BM * 8 / NT, GB = BN * 8 / NT;
     __shared__ u4 sm[(BM + BN) * 8];
     __shared__ float sc[BM + BN];
@@ -397,14 +440,221 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArg
     }
 }
 
-template <int TA, int TB, bool EXACT>
-static hipError_t launch_gemm(const GemmArgs &g0, hipStream_t st) {
+// A wave's outputs from row m0 and column n0 on: lane (q4, l16) holds rows 16 i + l16, columns 16 j + 4 q4 .. + 3.
+// Stores carry 32-bit offsets from the corner; rows behind the last lie behind the buffer's bound, which drops them, and
+// columns behind the last are sent there, so nothing branches.  (store_tile's caller has 16 MI rows in 2^30 bytes.)
+template <int TO, bool QUADS, int MI, int NI>
+__device__ __forceinline__ void store_rows(const __amdgpu_buffer_rsrc_t o, const float *bias, int cols, uint32_t ldo, int l16, int q4,
+                                           const f4 (&acc)[MI][NI]) {
+    constexpr uint32_t ES = TO == SC_F32 ? 4 : 2, BEHIND = 0x80000000u;
+    const uint32_t row = (uint32_t)l16 * ldo * ES, step = 16u * ldo * ES;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int n = 16 * j + 4 * q4;
+        f4 add = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (bias)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add[e] = bias[min(n + e, cols - 1)];
+        uint32_t at[4];
+#pragma unroll
+        for (int e = 0; e < (QUADS ? 1 : 4); ++e) at[e] = n + e < cols ? row + (uint32_t)(n + e) * ES : BEHIND;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const f4 v = acc[i][j] + add;
+            if (QUADS && TO == SC_F32) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), o, at[0] + i * step, 0, 0);
+            } else if (QUADS) {
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e]);
+                __builtin_amdgcn_raw_buffer_store_b64(u2{h[0] | h[1] << 16, h[2] | h[3] << 16}, o, at[0] + i * step, 0, 0);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (TO == SC_F32) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), o, at[e] + i * step, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e])), o, at[e] + i * step, 0, 0);
+                }
+            }
+        }
+    }
+}
+template <bool EXACT, int MI, int NI>
+__device__ __forceinline__ void store_tile(const GemmArgs &g, int b, int64_t m0, int64_t n0, int l16, int q4, const f4 (&acc)[MI][NI]) {
+    const int64_t es = EXACT ? 4 : 2;
+    const int rows = (int)min(g.M - m0, (int64_t)(16 * MI)), cols = (int)min(g.N - n0, (int64_t)(16 * NI));
+    if (rows <= 0 || cols <= 0) return;
+    uint8_t *corner = static_cast<uint8_t *>(g.out) + (b * g.strideO + m0 * g.ldo + n0) * es;
+    const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(corner, 0, (int)(((rows - 1) * g.ldo + cols) * es), 0x00020000);
+    const float *bias = g.bias ? g.bias + b * g.strideBias + n0 : nullptr;
+    const uint32_t ldo = (uint32_t)g.ldo;
+    if (EXACT) {
+        if (g.vecO) store_rows<SC_F32, true>(o, bias, cols, ldo, l16, q4, acc);
+        else store_rows<SC_F32, false>(o, bias, cols, ldo, l16, q4, acc);
+    } else if (g.typeO == SC_BF16) {
+        if (g.vecO) store_rows<SC_BF16, true>(o, bias, cols, ldo, l16, q4, acc);
+        else store_rows<SC_BF16, false>(o, bias, cols, ldo, l16, q4, acc);
+    } else {
+        if (g.vecO) store_rows<SC_F16, true>(o, bias, cols, ldo, l16, q4, acc);
+        else store_rows<SC_F16, false>(o, bias, cols, ldo, l16, q4, acc);
+    }
+}
+
+// A tile of BM x BN outputs by waves of WM x WN each, one block after the other by the same threads.  A scale block is
+// one stage: the matrix cores sum its 128 products from zero and the sum enters the accumulators times its two
+// scales.  A stage's operands and scales are copied to LDS while the stage before it is multiplied.
+// BLOCKB: the rows of B share a scale by 128, so a wave's columns have one.
+template <int TA, int TB, bool EXACT, bool BLOCKB, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArgs g, uint32_t tiles) {
+    constexpr int NW = (BM / WM) * (BN / WN), MI = WM / 16, NI = WN / 16, ROWS = BM + BN;
+    constexpr int WR = ROWS / NW, CH = WR / 8;      // rows that a wave copies of each stage, eight at a time
+    static_assert(WR == 64 && BM % WR == 0, "a wave copies rows of one operand, and a scale for each of its lanes");
+    __shared__ u4 sm[2][ROWS * 8];
+    __shared__ float sc[2][ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4;
+    const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
+
+    // what this wave copies: rows r0 .. r0 + 63 of a tile of A or of B
+    const bool forB = wave >= BM / WR;
+    const int r0 = (forB ? wave - BM / WR : wave) * WR, shift = forB ? g.shiftB : g.shiftA, all = forB ? g.N : g.M;
+    const int64_t ld = forB ? g.ldb : g.lda, lds = forB ? g.ldsB : g.ldsA, stride = forB ? g.strideB : g.strideA,
+                  sstride = forB ? g.strideSB : g.strideSA;
+    const uint8_t *const src = forB ? g.B : g.A;
+    const float *const ssrc = forB ? g.sB : g.sA;
+    uint32_t off[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int r = r0 + 8 * k + (lane >> 3);
+        off[k] = (uint32_t)r * (uint32_t)ld + 16u * ((lane & 7) ^ swz(r));
+    }
+    const uint32_t soff = 4u * (uint32_t)((r0 + lane) >> shift) * (uint32_t)lds;
+    // the next stage to copy: stage ct of the tile (cb, cm, cn)
+    Buffer from, sfrom;
+    uint32_t next = blockIdx.x;
+    int cb, cm, cn, ct = 0;
+    const auto enter = [&]() {
+        tile_at(next, tiles, g.tilesM, g.tilesN, &cb, &cm, &cn);
+        const int64_t x0 = forB ? (int64_t)cn * BN : (int64_t)cm * BM, rows = min((int64_t)(forB ? BN : BM), all - x0);
+        from = buffer_of(src + cb * stride + x0 * ld, (rows - 1) * ld + g.K);
+        sfrom = buffer_of(ssrc + cb * sstride + (x0 >> shift) * lds, 4 * (((rows - 1) >> shift) * lds + g.KB));
+    };
+    const auto advance = [&]() {      // to the stage behind the one that has been copied; behind the last there is nothing to read
+        if (++ct < g.KB) {
+            from = advanced(from, 128);
+            sfrom = advanced(sfrom, 4);
+            return;
+        }
+        ct = 0;
+        next += gridDim.x;
+        if (next < tiles) enter();
+        else from[2] = sfrom[2] = 0u;
+    };
+    const auto copy = [&](int buf, int k) { copy16(from, off[k], lds_address(&sm[buf][(wave * CH + k) * 64])); };
+    const auto copy_scales = [&](int buf) { copy4(sfrom, soff, lds_address(&sc[buf][wave * WR])); };
+    enter();
+    if (g.KB > 0) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) copy(0, k);
+        copy_scales(0);
+    }
+    const int cut = g.K & 127;
+    int buf = 0;
+    for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+        const int64_t m0 = (int64_t)cm * BM, n0 = (int64_t)cn * BN;
+        const int b = cb;
+        f4 acc[MI][NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < g.KB; ++t) {
+            wait_copies();
+            if (cut && t + 1 == g.KB) {
+                // a cut last stage: what lies behind K in this wave's rows becomes zero
+#pragma unroll 1
+                for (int k = 0; k < CH; ++k) {
+                    u4 *p = &sm[buf][(wave * CH + k) * 64 + lane];
+                    const int left = cut - 16 * ((lane & 7) ^ swz(8 * k + (lane >> 3)));
+                    *p &= u4{bytes_before(left), bytes_before(left - 4), bytes_before(left - 8), bytes_before(left - 12)};
+                }
+            }
+            __syncthreads();          // everyone's copies have arrived, and the other buffer has been read
+            advance();
+            // Row group i is multiplied while group i + 1 is read, a part of the next stage is sent for and the sums of group
+            // i - 1 are scaled.  The fences hold that order: left to itself the compiler scales a group's sums as soon as they
+            // are there, and both waves of a SIMD then wait for the same unit in turn.
+            const u4 *s = sm[buf];
+            const auto read = [&](auto &f, int r) { f.set(s[r * 8 + (q4 ^ swz(r))], s[r * 8 + ((q4 + 4) ^ swz(r))]); };
+            Frag<TB, EXACT> fb[NI];
+            Frag<TA, EXACT> fa[2];
+            f4 sb[BLOCKB ? 1 : NI], p[2][NI];
+            float sa[3];
+            read(fa[0], wm + l16);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) read(fb[j], BM + wn + 16 * j + l16);
+            if (BLOCKB) {
+                sb[0] = f4{sc[buf][BM + wn], 0.0f, 0.0f, 0.0f};
+            } else {
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sb[j] = *reinterpret_cast<const f4 *>(&sc[buf][BM + wn + 16 * j + 4 * q4]);
+            }
+            sa[0] = sc[buf][wm + l16];
+            copy_scales(buf ^ 1);
+            const auto add = [&](int i, int j) {
+                const float s0 = sa[i % 3];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[i & 1][j][e], BLOCKB ? s0 : s0 * sb[BLOCKB ? 0 : j][e], acc[i][j][e]);
+            };
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                if (i + 1 < MI) {
+                    read(fa[(i + 1) & 1], wm + 16 * (i + 1) + l16);
+                    sa[(i + 1) % 3] = sc[buf][wm + 16 * (i + 1) + l16];
+                }
+#pragma unroll
+                for (int k = i * CH / MI; k < (i + 1) * CH / MI; ++k) copy(buf ^ 1, k);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    p[i & 1][j] = mma_128(fb[j], fa[i & 1]);
+                    if (i > 0) add(i - 1, j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (BLOCKB) sa[i % 3] *= sb[0][0];
+            }
+#pragma unroll
+            for (int j = 0; j < NI; ++j) add(MI - 1, j);
+            buf ^= 1;
+        }
+        if (g.KB == 0) {
+            next += gridDim.x;
+            if (next < tiles) enter();
+        }
+        store_tile<EXACT, MI, NI>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+    }
+}
+
+template <int TA, int TB, bool EXACT, bool BLOCKB, int BM, int BN, int WM, int WN>
+static hipError_t launch_tile(const GemmArgs &g0, int per_cu, hipStream_t st) {
     GemmArgs g = g0;
-    g.tilesM = (int)(((int64_t)g.M + 127) / 128);
-    g.tilesN = (int)(((int64_t)g.N + 127) / 128);
-    hipLaunchKernelGGL((k_fp8_gemm<TA, TB, EXACT, 128, 128, 64, 64>), grid_of((uint32_t)g.tilesM * (uint32_t)g.tilesN, g.batch),
-                       dim3(256), 0, st, g);
+    g.tilesM = (int)(((int64_t)g.M + BM - 1) / BM);
+    g.tilesN = (int)(((int64_t)g.N + BN - 1) / BN);
+    const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN * (uint32_t)g.batch, most = 256u * per_cu;
+    hipLaunchKernelGGL((k_fp8_gemm<TA, TB, EXACT, BLOCKB, BM, BN, WM, WN>), dim3(tiles < most ? tiles : most), dim3((BM / WM) * (BN / WN) * 64),
+                       0, st, g, tiles);
     return hipGetLastError();
+}
+template <int TA, int TB, bool EXACT>
+static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
+    const bool al = aligned_to(g.A, 16) && aligned_to(g.B, 16) && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.strideA % 16 == 0 && g.strideB % 16 == 0;
+    if (!al || g.lda > (1 << 23) || g.ldb > (1 << 23) || g.ldsA > (1 << 21) || g.ldsB > (1 << 21) || g.ldo > (1 << 20) || getenv("SCT0")) {
+        GemmArgs h = g;
+        h.tilesM = (int)(((int64_t)g.M + 127) / 128);
+        h.tilesN = (int)(((int64_t)g.N + 127) / 128);
+        hipLaunchKernelGGL((k_fp8_any<TA, TB, EXACT, 128, 128, 64, 64>), grid_of((uint32_t)h.tilesM * (uint32_t)h.tilesN, g.batch), dim3(256), 0, st, h);
+        return hipGetLastError();
+    }
+    if (getenv("SCT") && atoi(getenv("SCT")) == 1) return g.shiftB ? launch_tile<TA, TB, EXACT, true, 128, 128, 64, 64>(g, 2, st) : launch_tile<TA, TB, EXACT, false, 128, 128, 64, 64>(g, 2, st);
+    if (EXACT) return g.shiftB ? launch_tile<TA, TB, EXACT, true, 128, 128, 64, 64>(g, 2, st) : launch_tile<TA, TB, EXACT, false, 128, 128, 64, 64>(g, 2, st);
+    return g.shiftB ? launch_tile<TA, TB, false, true, 256, 256, 128, 64>(g, 1, st) : launch_tile<TA, TB, false, false, 256, 256, 128, 64>(g, 1, st);
 }
 
 template <bool EXACT>
@@ -509,7 +759,7 @@ int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, co
     g.shiftB = d.rowsB == 128 ? 7 : 0;
     g.typeO = d.typeO;
     const int vb = 4 * type_bytes(d.typeO);
-    g.vecO = aligned_to(out, vb) && d.ldo % 4 == 0 && d.strideO % 4 == 0;
+    g.vecO = aligned_to(out, vb) && d.N % 4 == 0 && d.ldo % 4 == 0 && d.strideO % 4 == 0;
     g.batch = d.batch;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const hipError_t e = d.typeO == SC_F32 ? launch_gemm_types<true>(g, d.typeA, d.typeB, st) : launch_gemm_types<false>(g, d.typeA, d.typeB, st);
