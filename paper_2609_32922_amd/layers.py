@@ -8,10 +8,12 @@ by it when it is another.
 """
 from __future__ import annotations
 
+import ctypes
+
 from ._lib import (SC_BF16, SC_BLOCK_1X128, SC_BLOCK_128X1_T, SC_BLOCK_128X128, SC_E4M3, SC_E5M2, SC_F16, SC_F32, SC_FP8_BLOCK,
                    SC_INT8, SC_NORM_LAYER, SC_NORM_NONE, SC_NORM_RMS, SC_OK, SC_ROPE_HALVES, SC_ROPE_NEIGHBOURS, ScError,
-                   ScFp8GemmDesc, ScNormDesc, ScRopeDesc, sc_fp8_gemm, sc_fp8_gemm_workspace_size, sc_fp8_quantize,
-                   sc_residual_norm, sc_residual_norm_backward, sc_residual_norm_backward_workspace_size, sc_rope)
+                   ScFp8GemmDesc, ScNormDesc, ScRopeDesc, load, sc_fp8_gemm_workspace_size,
+                   sc_residual_norm_backward_workspace_size)
 
 _types = {}
 
@@ -29,6 +31,70 @@ def _type(t, name, allowed):
 
 
 FLOATS, FP8 = (SC_F32, SC_BF16, SC_F16), (SC_E4M3, SC_E5M2)
+
+# The kernels of a small call take less time than checking its arguments in Python, so what the shapes, strides, types and
+# options of a call come to (the checks passed, the filled descriptor, what its results look like) is kept for the next call
+# with the same ones.  Nothing of the tensors themselves is.
+_PLANS_MOST = 1024
+_plans = {}
+
+
+def _keep(key, plan):
+    if len(_plans) >= _PLANS_MOST:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _form(t):
+    return (t.shape, t.stride(), t.dtype, t.device) if t is not None else None
+
+
+class _Plan:
+    """A checked call: its device, and the library's function with the arguments that do not change."""
+
+    def __init__(self, dev, name):
+        if dev.type != "cuda":
+            raise ValueError("tensors must be on a GPU")
+        self.dev, self.index, self.name = dev, dev.index, name
+        self.function = getattr(load(), name)
+
+    def stream(self, stream):
+        """(handle, the stream if tensors made here are used on another one than their own)"""
+        import torch
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.index), None
+        return int(stream.cuda_stream), stream if stream != torch.cuda.current_stream(self.dev) else None
+
+    def run(self, *args):
+        import torch
+        if torch._C._cuda_getDevice() == self.index:
+            rc = self.function(*args)
+        else:
+            with torch.cuda.device(self.dev):
+                rc = self.function(*args)
+        if rc != SC_OK:
+            raise ScError(rc, self.name)
+
+
+def _used_on(stream, *tensors):
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
+def _workspace(dev, nbytes, given, other):
+    """(address, bytes, what holds it) of a workspace; ``given`` is grown where it is too small."""
+    import torch
+    if given is not None:
+        given.ensure(nbytes)
+        if other is not None:
+            given._buf.record_stream(other)
+        return given.ptr, given.nbytes, given
+    buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
+    if other is not None:
+        buf.record_stream(other)
+    return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
 
 
 def _on(t, name, dev):
@@ -50,49 +116,23 @@ def _rows(t, name, dev, shape=None):
     return ld, t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0
 
 
-class _Call:
-    """Device, stream and outputs of one call."""
-
-    def __init__(self, dev, stream):
-        import torch
-        if dev.type != "cuda":
-            raise ValueError("tensors must be on a GPU")
-        self.dev, self.stream, self.torch = dev, stream, torch
-        self.foreign = stream is not None and stream != torch.cuda.current_stream(dev)
-        self.handle = int(stream.cuda_stream) if stream is not None else torch._C._cuda_getCurrentRawStream(dev.index)
-
-    def empty(self, shape, dtype):
-        t = self.torch.empty(shape, dtype=dtype, device=self.dev)
-        if self.foreign:
-            t.record_stream(self.stream)
-        return t
-
-    def workspace(self, nbytes, given=None):
-        """(address, bytes) of a workspace; ``given`` is grown where it is too small."""
-        if nbytes == 0:
-            return 0, 0
-        if given is None:
-            from . import Workspace
-            given = Workspace(nbytes, self.dev)
-        else:
-            given.ensure(nbytes)
-        if self.foreign:
-            given._buf.record_stream(self.stream)
-        return given.ptr, given.nbytes
-
-    def run(self, function, name, *args):
-        cuda = self.torch.cuda
-        if self.dev.index != cuda.current_device():
-            with cuda.device(self.dev):
-                rc = function(*args, self.handle)
-        else:
-            rc = function(*args, self.handle)
-        if rc != SC_OK:
-            raise ScError(rc, name)
-
-
 def _ptr(t):
-    return t.data_ptr() if t is not None else 0
+    return t.data_ptr() if t is not None else None
+
+
+def _quantize_plan(key, X, dtype, block):
+    import torch
+    p = _Plan(X.device, "sc_fp8_quantize")
+    ld, st = _rows(X, "X", p.dev)
+    tx, tq = _type(X.dtype, "X", FLOATS), _type(dtype, "dtype", FP8)
+    lead, (rows, K) = tuple(X.shape[:-2]), X.shape[-2:]
+    kb, rb = -(-K // SC_FP8_BLOCK), -(-rows // SC_FP8_BLOCK)
+    turned = block == SC_BLOCK_128X1_T
+    qs, ss = ((K, rows), (K, rb)) if turned else ((rows, K), (rb if block == SC_BLOCK_128X128 else rows, kb))
+    p.q_shape, p.s_shape, p.f32 = lead + qs, lead + ss, torch.float32
+    p.head, p.mid = (lead[0] if lead else 1, rows, K, tx), (ld, st, tq, block)
+    p.q_strides, p.s_strides = (qs[1], qs[0] * qs[1]), (ss[1], ss[0] * ss[1])
+    return _keep(key, p)
 
 
 def fp8_quantize(X, *, dtype=None, block: int = SC_BLOCK_1X128, stream=None):
@@ -103,18 +143,15 @@ def fp8_quantize(X, *, dtype=None, block: int = SC_BLOCK_1X128, stream=None):
     transpose's rows, Q [.., K, rows] and scale [.., K, ceil(rows/128)].
     """
     import torch
-    dtype = torch.float8_e4m3fn if dtype is None else dtype
-    c = _Call(X.device, stream)
-    ld, st = _rows(X, "X", c.dev)
-    tx, tq = _type(X.dtype, "X", FLOATS), _type(dtype, "dtype", FP8)
-    lead, (rows, K) = tuple(X.shape[:-2]), X.shape[-2:]
-    batch = lead[0] if lead else 1
-    kb, rb = -(-K // SC_FP8_BLOCK), -(-rows // SC_FP8_BLOCK)
-    turned = block == SC_BLOCK_128X1_T
-    qs, ss = ((K, rows), (K, rb)) if turned else ((rows, K), (rb if block == SC_BLOCK_128X128 else rows, kb))
-    Q, scale = c.empty(lead + qs, dtype), c.empty(lead + ss, torch.float32)
-    c.run(sc_fp8_quantize, "sc_fp8_quantize", batch, rows, K, tx, X.data_ptr(), ld, st, tq, block, Q.data_ptr(), qs[1],
-          qs[0] * qs[1], scale.data_ptr(), ss[1], ss[0] * ss[1])
+    if dtype is None:
+        dtype = torch.float8_e4m3fn
+    key = ("quantize", X.shape, X.stride(), X.dtype, X.device, dtype, block)
+    p = _plans.get(key) or _quantize_plan(key, X, dtype, block)
+    Q, scale = torch.empty(p.q_shape, dtype=dtype, device=p.dev), torch.empty(p.s_shape, dtype=p.f32, device=p.dev)
+    handle, other = p.stream(stream)
+    if other is not None:
+        _used_on(other, Q, scale)
+    p.run(*p.head, X.data_ptr(), *p.mid, Q.data_ptr(), *p.q_strides, scale.data_ptr(), *p.s_strides, handle)
     return Q, scale
 
 
@@ -128,52 +165,69 @@ def _scale_rows(s, name, dev, rows, kb, lead):
     return per, ld, st
 
 
-def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
-    """out = (sA . A) (sB . B)^T (+ bias) of 8-bit floats with a scale for each block of 128 elements of a row.
-
-    A [M, K] or [batch, M, K], B [N, K] or [batch or 1, N, K] (torch.float8_e4m3fn or float8_e5m2 each); sA float32
-    [.., M, ceil(K/128)] or [.., ceil(M/128), ceil(K/128)], sB alike, as ``fp8_quantize`` gives them; bias float32 [N] or
-    [batch, N].  ``out_dtype`` (default bfloat16) or ``out`` with rows of any stride.  Returns out [.., M, N].
-    """
+def _gemm_plan(key, A, sA, B, sB, bias, out, out_dtype):
     import torch
-    c = _Call(A.device, stream)
+    p = _Plan(A.device, "sc_fp8_gemm")
     d = ScFp8GemmDesc()
     d.typeA, d.typeB = _type(A.dtype, "A", FP8), _type(B.dtype, "B", FP8)
-    d.lda, d.strideA = _rows(A, "A", c.dev)
+    d.lda, d.strideA = _rows(A, "A", p.dev)
     lead, (M, K) = tuple(A.shape[:-2]), A.shape[-2:]
     batch = lead[0] if lead else 1
-    d.ldb, d.strideB = _rows(B, "B", c.dev)
+    d.ldb, d.strideB = _rows(B, "B", p.dev)
     N = B.shape[-2]
     leadB = tuple(B.shape[:-2])
     if B.shape[-1] != K or (leadB and leadB[0] not in (1, batch)):
         raise ValueError("A is [batch, M, K], B must be [batch or 1, N, K]")
     kb = -(-K // SC_FP8_BLOCK)
-    d.rowsA, d.ldsA, d.strideSA = _scale_rows(sA, "sA", c.dev, M, kb, lead)
-    d.rowsB, d.ldsB, d.strideSB = _scale_rows(sB, "sB", c.dev, N, kb, leadB)
+    d.rowsA, d.ldsA, d.strideSA = _scale_rows(sA, "sA", p.dev, M, kb, lead)
+    d.rowsB, d.ldsB, d.strideSB = _scale_rows(sB, "sB", p.dev, N, kb, leadB)
     d.batch, d.M, d.N, d.K = batch, M, N, K
     if bias is not None:
-        _on(bias, "bias", c.dev)
+        _on(bias, "bias", p.dev)
         if bias.dtype != torch.float32:
             raise TypeError("bias must be float32")
         if tuple(bias.shape) not in ((N,), (batch, N)) or (N > 1 and bias.stride(-1) != 1):
             raise ValueError("bias must be [N] or [batch, N] with a contiguous last dimension")
         d.strideBias = bias.stride(0) if bias.dim() == 2 and batch > 1 else 0
+    p.shape, p.dtype = lead + (M, N), torch.bfloat16 if out_dtype is None else out_dtype
     if out is None:
-        out = c.empty(lead + (M, N), torch.bfloat16 if out_dtype is None else out_dtype)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError("out must be %s" % out_dtype)
-    d.typeO = _type(out.dtype, "out", FLOATS)
-    d.ldo, d.strideO = _rows(out, "out", c.dev, lead + (M, N))
-    ws, nbytes = c.workspace(sc_fp8_gemm_workspace_size(d), workspace)
-    c.run(sc_fp8_gemm, "sc_fp8_gemm", d, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), _ptr(bias), out.data_ptr(),
-          ws, nbytes)
+        d.typeO = _type(p.dtype, "out", FLOATS)
+        d.ldo, d.strideO = max(N, 1), M * N
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError("out must be %s" % out_dtype)
+        d.typeO = _type(out.dtype, "out", FLOATS)
+        d.ldo, d.strideO = _rows(out, "out", p.dev, p.shape)
+    p.nbytes, p.desc, p.ref = sc_fp8_gemm_workspace_size(d), d, ctypes.byref(d)
+    return _keep(key, p)
+
+
+def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=None, stream=None):
+    """out = (sA . A) (sB . B)^T (+ bias) of 8-bit floats with a scale for each block of 128 elements of a row.
+
+    A [M, K] or [batch, M, K], B [N, K] or [batch or 1, N, K] (torch.float8_e4m3fn or float8_e5m2 each); sA float32
+    [.., M, ceil(K/128)] or [.., ceil(M/128), ceil(K/128)], sB alike, as ``fp8_quantize`` gives them; bias float32 [N] or
+    [batch, N].  ``out_dtype`` (default bfloat16) or ``out`` with rows of any stride.  float32 results have float32 products
+    and sums throughout; 16-bit ones take the matrix cores' 8-bit products.  Returns out [.., M, N].
+    """
+    import torch
+    key = ("gemm", A.shape, A.stride(), A.dtype, A.device, sA.shape, sA.stride(), sA.dtype, sA.device, B.shape, B.stride(), B.dtype,
+           B.device, sB.shape, sB.stride(), sB.dtype, sB.device, out_dtype, _form(bias), _form(out))
+    p = _plans.get(key) or _gemm_plan(key, A, sA, B, sB, bias, out, out_dtype)
+    handle, other = p.stream(stream)
+    if out is None:
+        out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
+        if other is not None:
+            out.record_stream(other)
+    ws = (None, 0, None) if p.nbytes == 0 else _workspace(p.dev, p.nbytes, workspace, other)
+    p.run(p.ref, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), _ptr(bias), out.data_ptr(), ws[0], ws[1], handle)
     return out
 
 
 _PARAMS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
 
 
-def _norm_desc(c, x, y, dtype_h, post, pre, post_eps, pre_eps, res_scale, post_offset, pre_offset, params):
+def _norm_desc(c, x, y, dtype_h, post, pre, numbers, params):
     d = ScNormDesc()
     d.batch = x.shape[0] if x.dim() == 3 else 1
     d.rows, d.D = x.shape[-2:]
@@ -181,7 +235,7 @@ def _norm_desc(c, x, y, dtype_h, post, pre, post_eps, pre_eps, res_scale, post_o
     d.typeX = _type(x.dtype, "x", FLOATS)
     d.typeY = _type(y.dtype, "y", FLOATS) if y is not None else d.typeX
     d.typeH = dtype_h
-    d.eps_post, d.eps_pre, d.scale_res, d.off_post, d.off_pre = post_eps, pre_eps, res_scale, post_offset, pre_offset
+    d.eps_post, d.eps_pre, d.scale_res, d.off_post, d.off_pre = numbers
     D, batch = d.D, d.batch
     d.ldx = d.ldy = d.ldxo = d.ldh = max(D, 1)
     d.lds = -(-D // SC_FP8_BLOCK)
@@ -203,6 +257,29 @@ def _norm_desc(c, x, y, dtype_h, post, pre, post_eps, pre_eps, res_scale, post_o
     return d
 
 
+def _norm_plan(key, x, y, params, post, pre, numbers, out_dtype, want_x, want_h, want_rowmax, inplace):
+    import torch
+    p = _Plan(x.device, "sc_residual_norm")
+    th = _type(out_dtype, "out_dtype", FLOATS + FP8 + (SC_INT8,))
+    ldx, sx = _rows(x, "x", p.dev)
+    d = _norm_desc(p, x, y, th, post, pre, numbers, params)
+    d.ldx, d.strideX = ldx, sx
+    if y is not None:
+        d.ldy, d.strideY = _rows(y, "y", p.dev, x.shape)
+    lead, D = tuple(x.shape[:-1]), d.D
+    if inplace and not want_x:
+        raise ValueError("inplace writes xo: want_x must be set")
+    if want_rowmax and not (want_h and th == SC_INT8):
+        raise ValueError("rowmax comes with an int8 h")
+    d.ldxo, d.strideXO = (ldx, sx) if inplace else (max(D, 1), d.rows * D)
+    d.ldh, d.strideH = max(D, 1), d.rows * D
+    d.strideS = d.rows * d.lds if th in FP8 else d.rows
+    p.shape, p.h_dtype, p.f32 = tuple(x.shape), out_dtype, torch.float32
+    p.s_shape = None if not want_h or th in FLOATS else lead if th == SC_INT8 else lead + (d.lds,)
+    p.desc, p.ref = d, ctypes.byref(d)
+    return _keep(key, p)
+
+
 def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAYER, post_weight=None, post_bias=None,
                   gate=None, pre_weight=None, pre_bias=None, res_scale: float = 1.0, post_offset: float = 0.0,
                   pre_offset: float = 0.0, post_eps: float = 1e-6, pre_eps: float = 1e-6, out_dtype=None, want_x: bool = True,
@@ -217,36 +294,56 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
     there.
     """
     import torch
-    c = _Call(x.device, stream)
-    out_dtype = x.dtype if out_dtype is None else out_dtype
-    th = _type(out_dtype, "out_dtype", FLOATS + FP8 + (SC_INT8,))
-    params = (post_weight, post_bias, gate, pre_weight, pre_bias)
-    ldx, sx = _rows(x, "x", c.dev)
-    d = _norm_desc(c, x, y, th, post, pre, post_eps, pre_eps, res_scale, post_offset, pre_offset, params)
-    d.ldx, d.strideX = ldx, sx
-    if y is not None:
-        d.ldy, d.strideY = _rows(y, "y", c.dev, x.shape)
-    lead, D = tuple(x.shape[:-1]), d.D
-    xo = None
-    if want_x:
-        xo = x if inplace else c.empty(lead + (D,), x.dtype)
-        d.ldxo, d.strideXO = _rows(xo, "xo", c.dev)
-    elif inplace:
-        raise ValueError("inplace writes xo: want_x must be set")
-    h = scale = rowmax = None
-    if want_h:
-        h = c.empty(lead + (D,), out_dtype)
-        d.ldh, d.strideH = _rows(h, "h", c.dev)
-        if th == SC_INT8:
-            scale, d.strideS = c.empty(lead, torch.float32), d.rows
-            rowmax = c.empty(lead, torch.float32) if want_rowmax else None
-        elif th in FP8:
-            scale, d.strideS = c.empty(lead + (d.lds,), torch.float32), d.rows * d.lds
-    if want_rowmax and rowmax is None:
-        raise ValueError("rowmax comes with an int8 h")
-    c.run(sc_residual_norm, "sc_residual_norm", d, x.data_ptr(), _ptr(y), *(_ptr(p) for p in params), _ptr(xo), _ptr(h),
-          _ptr(scale), _ptr(rowmax))
+    if out_dtype is None:
+        out_dtype = x.dtype
+    key = ("norm", x.shape, x.stride(), x.dtype, x.device, _form(y), _form(post_weight), _form(post_bias), _form(gate),
+           _form(pre_weight), _form(pre_bias), post, pre, res_scale, post_offset, pre_offset, post_eps, pre_eps, out_dtype, want_x,
+           want_h, want_rowmax, inplace)
+    p = _plans.get(key) or _norm_plan(key, x, y, (post_weight, post_bias, gate, pre_weight, pre_bias), post, pre,
+                                      (post_eps, pre_eps, res_scale, post_offset, pre_offset), out_dtype, want_x, want_h,
+                                      want_rowmax, inplace)
+    dev = p.dev
+    xo = None if not want_x else x if inplace else torch.empty(p.shape, dtype=x.dtype, device=dev)
+    h = torch.empty(p.shape, dtype=out_dtype, device=dev) if want_h else None
+    scale = torch.empty(p.s_shape, dtype=p.f32, device=dev) if p.s_shape is not None else None
+    rowmax = torch.empty(p.s_shape, dtype=p.f32, device=dev) if want_rowmax else None
+    handle, other = p.stream(stream)
+    if other is not None:
+        _used_on(other, None if inplace else xo, h, scale, rowmax)
+    p.run(p.ref, x.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight), _ptr(pre_bias), _ptr(xo),
+          _ptr(h), _ptr(scale), _ptr(rowmax), handle)
     return xo, h, scale, rowmax
+
+
+def _backward_plan(key, xo, y, dxo, dh, params, post, pre, numbers, want_x, want_params):
+    p = _Plan(xo.device, "sc_residual_norm_backward")
+    th = _type(dh.dtype, "dh", FLOATS) if dh is not None else SC_F32
+    ldxo, sxo = _rows(xo, "xo", p.dev)
+    d = _norm_desc(p, xo, y, th, post, pre, numbers, params)
+    D = max(d.D, 1)
+    d.ldxo, d.strideXO = ldxo, sxo
+    if y is not None:
+        d.ldy, d.strideY = _rows(y, "y", p.dev, xo.shape)
+    elif post != SC_NORM_NONE or any(q is not None for q in params[:3]):
+        raise ValueError("a branch's norm and gate need y")
+    if dxo is not None:
+        if dxo.dtype != xo.dtype:
+            raise TypeError("dxo must have xo's type")
+        d.lddxo, d.strideDXO = _rows(dxo, "dxo", p.dev, xo.shape)
+    if dh is not None:
+        d.ldh, d.strideH = _rows(dh, "dh", p.dev, xo.shape)
+    d.ldx = d.lddy = D
+    d.strideX = d.strideDY = d.rows * d.D
+    p.shape = tuple(xo.shape)
+    # the parameters' gradients, made together by their shapes
+    p.sums = {}
+    if want_params:
+        for name, q in zip(_PARAMS, params):
+            if q is not None:
+                p.sums.setdefault(tuple(q.shape), []).append(name)
+    p.nbytes = sc_residual_norm_backward_workspace_size(d) if p.sums else 0
+    p.desc, p.ref = d, ctypes.byref(d)
+    return _keep(key, p)
 
 
 def residual_norm_backward(xo, y=None, *, dxo=None, dh=None, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAYER,
@@ -261,39 +358,27 @@ def residual_norm_backward(xo, y=None, *, dxo=None, dh=None, post: int = SC_NORM
     the parameter's shape (summed over the rows, and over the batch where it is shared).
     """
     import torch
-    c = _Call(xo.device, stream)
-    params = (post_weight, post_bias, gate, pre_weight, pre_bias)
-    th = _type(dh.dtype, "dh", FLOATS) if dh is not None else SC_F32
-    ldxo, sxo = _rows(xo, "xo", c.dev)
-    d = _norm_desc(c, xo, y, th, post, pre, post_eps, pre_eps, res_scale, post_offset, pre_offset, params)
-    d.ldxo, d.strideXO = ldxo, sxo
-    if y is not None:
-        d.ldy, d.strideY = _rows(y, "y", c.dev, xo.shape)
-    elif post != SC_NORM_NONE or any(p is not None for p in params[:3]):
-        raise ValueError("a branch's norm and gate need y")
-    if dxo is not None:
-        if dxo.dtype != xo.dtype:
-            raise TypeError("dxo must have xo's type")
-        d.lddxo, d.strideDXO = _rows(dxo, "dxo", c.dev, xo.shape)
-    if dh is not None:
-        d.ldh, d.strideH = _rows(dh, "dh", c.dev, xo.shape)
+    key = ("back", xo.shape, xo.stride(), xo.dtype, xo.device, _form(y), _form(dxo), _form(dh), _form(post_weight), _form(post_bias),
+           _form(gate), _form(pre_weight), _form(pre_bias), post, pre, res_scale, post_offset, pre_offset, post_eps, pre_eps, want_x,
+           want_params)
+    p = _plans.get(key) or _backward_plan(key, xo, y, dxo, dh, (post_weight, post_bias, gate, pre_weight, pre_bias), post, pre,
+                                          (post_eps, pre_eps, res_scale, post_offset, pre_offset), want_x, want_params)
+    dev = p.dev
+    handle, other = p.stream(stream)
     got = {}
-    dx = dy = None
     if want_x:
-        dx = got["x"] = c.empty(tuple(xo.shape), xo.dtype)
-        d.ldx, d.strideX = _rows(dx, "dx", c.dev)
+        got["x"] = torch.empty(p.shape, dtype=xo.dtype, device=dev)
     if y is not None:
-        dy = got["y"] = c.empty(tuple(y.shape), y.dtype)
-        d.lddy, d.strideDY = _rows(dy, "dy", c.dev)
-    sums = []
-    for name, p in zip(_PARAMS, params):
-        g = None
-        if p is not None and want_params:
-            g = got[name] = c.empty(tuple(p.shape), torch.float32)
-        sums.append(g)
-    ws, nbytes = c.workspace(sc_residual_norm_backward_workspace_size(d) if any(g is not None for g in sums) else 0, workspace)
-    c.run(sc_residual_norm_backward, "sc_residual_norm_backward", d, xo.data_ptr(), _ptr(y), *(_ptr(p) for p in params[:4]),
-          _ptr(dxo), _ptr(dh), _ptr(dx), _ptr(dy), *(_ptr(g) for g in sums), ws, nbytes)
+        got["y"] = torch.empty(p.shape, dtype=y.dtype, device=dev)
+    for shape, names in p.sums.items():
+        got.update(zip(names, torch.empty((len(names),) + shape, dtype=torch.float32, device=dev).unbind(0)))
+    if other is not None:
+        _used_on(other, *got.values())
+    ws = (None, 0, None) if p.nbytes == 0 else _workspace(dev, p.nbytes, workspace, other)
+    g = got.get
+    p.run(p.ref, xo.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight), _ptr(dxo), _ptr(dh),
+          _ptr(g("x")), _ptr(g("y")), _ptr(g("post_weight")), _ptr(g("post_bias")), _ptr(g("gate")), _ptr(g("pre_weight")),
+          _ptr(g("pre_bias")), ws[0], ws[1], handle)
     return got
 
 
@@ -325,15 +410,16 @@ def _heads(t, name, dev):
     return (t.stride(0) if t.dim() == 4 else 0), t.stride(-3), t.stride(-2)
 
 
-def _rope(c, x, pos, freq, axis, interleaved, inverse):
+def _rope_plan(key, x, pos, freq, axis, interleaved, inverse, out, out_dtype, quantised):
     import torch
+    p = _Plan(x.device, "sc_rope")
     d = ScRopeDesc()
-    d.strideXB, d.strideXT, d.strideXH = _heads(x, "x", c.dev)
+    d.strideXB, d.strideXT, d.strideXH = _heads(x, "x", p.dev)
     d.batch = x.shape[0] if x.dim() == 4 else 1
     d.tokens, d.heads, d.D = x.shape[-3:]
     d.typeX = _type(x.dtype, "x", FLOATS)
     for t, name, dtype in ((pos, "pos", torch.int32), (freq, "freq", torch.float64), (axis, "axis", torch.int32)):
-        _on(t, name, c.dev)
+        _on(t, name, p.dev)
         if t.dtype != dtype:
             raise TypeError("%s must be %s" % (name, dtype))
     if freq.dim() != 1 or axis.shape != freq.shape or not freq.is_contiguous() or not axis.is_contiguous():
@@ -347,7 +433,23 @@ def _rope(c, x, pos, freq, axis, interleaved, inverse):
     d.stridePA = pos.stride(-2)
     d.pairing = SC_ROPE_NEIGHBOURS if interleaved else SC_ROPE_HALVES
     d.inverse = 1 if inverse else 0
-    return d
+    H, T, D = d.heads, d.tokens, d.D
+    if quantised:
+        p.shape, p.s_shape = tuple(x.shape[:-3]) + (H, T, D), tuple(x.shape[:-3]) + (H, T)
+        d.typeO = SC_INT8
+        d.strideOB, d.strideOT, d.strideOH = H * T * D, D, T * D
+        d.strideSB, d.strideST, d.strideSH = H * T, 1, T
+    elif out is None:
+        p.shape, p.dtype = tuple(x.shape), x.dtype if out_dtype is None else out_dtype
+        d.typeO = _type(p.dtype, "out", FLOATS)
+        d.strideOB, d.strideOT, d.strideOH = T * H * D, H * D, D
+    else:
+        if tuple(out.shape) != tuple(x.shape) or (out_dtype is not None and out.dtype != out_dtype):
+            raise ValueError("out must be like x, of out_dtype")
+        d.typeO = _type(out.dtype, "out", FLOATS)
+        d.strideOB, d.strideOT, d.strideOH = _heads(out, "out", p.dev)
+    p.desc, p.ref = d, ctypes.byref(d)
+    return _keep(key, p)
 
 
 def rope(x, pos, freq, axis, *, interleaved: bool = False, inverse: bool = False, out=None, out_dtype=None, stream=None):
@@ -358,15 +460,16 @@ def rope(x, pos, freq, axis, *, interleaved: bool = False, inverse: bool = False
     Pairs are elements (p, pairs + p), or (2p, 2p + 1) where ``interleaved``; elements behind them pass.  ``inverse`` turns
     back: the gradient of x from that of the result.  ``out`` may be x itself.  Returns out, like x.
     """
-    c = _Call(x.device, stream)
-    d = _rope(c, x, pos, freq, axis, interleaved, inverse)
+    import torch
+    key = ("rope", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
+           freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved, inverse, out_dtype, _form(out))
+    p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, inverse, out, out_dtype, False)
+    handle, other = p.stream(stream)
     if out is None:
-        out = c.empty(tuple(x.shape), x.dtype if out_dtype is None else out_dtype)
-    elif tuple(out.shape) != tuple(x.shape) or (out_dtype is not None and out.dtype != out_dtype):
-        raise ValueError("out must be like x, of out_dtype")
-    d.typeO = _type(out.dtype, "out", FLOATS)
-    d.strideOB, d.strideOT, d.strideOH = _heads(out, "out", c.dev)
-    c.run(sc_rope, "sc_rope", d, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), out.data_ptr(), 0, 0)
+        out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
+        if other is not None:
+            out.record_stream(other)
+    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), out.data_ptr(), None, None, handle)
     return out
 
 
@@ -376,16 +479,14 @@ def rope_quantize(x, pos, freq, axis, *, interleaved: bool = False, want_rowmax:
     Returns (Q int8 [.., heads, tokens, D], scale float32 [.., heads, tokens], rowmax alike or None).
     """
     import torch
-    c = _Call(x.device, stream)
-    d = _rope(c, x, pos, freq, axis, interleaved, False)
-    lead = tuple(x.shape[:-3])
-    H, T, D = d.heads, d.tokens, d.D
-    Q = c.empty(lead + (H, T, D), torch.int8)
-    scale = c.empty(lead + (H, T), torch.float32)
-    rowmax = c.empty(lead + (H, T), torch.float32) if want_rowmax else None
-    d.typeO = SC_INT8
-    d.strideOB, d.strideOT, d.strideOH = H * T * D, D, T * D
-    d.strideSB, d.strideST, d.strideSH = H * T, 1, T
-    c.run(sc_rope, "sc_rope", d, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), Q.data_ptr(),
-          scale.data_ptr(), _ptr(rowmax))
+    key = ("rope int8", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
+           freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved)
+    p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, False, None, None, True)
+    Q = torch.empty(p.shape, dtype=torch.int8, device=p.dev)
+    scale = torch.empty(p.s_shape, dtype=torch.float32, device=p.dev)
+    rowmax = torch.empty(p.s_shape, dtype=torch.float32, device=p.dev) if want_rowmax else None
+    handle, other = p.stream(stream)
+    if other is not None:
+        _used_on(other, Q, scale, rowmax)
+    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), Q.data_ptr(), scale.data_ptr(), _ptr(rowmax), handle)
     return Q, scale, rowmax
