@@ -297,7 +297,7 @@ int sc_fp8_gemm_workspace_size(const sc_fp8_gemm_desc *desc, size_t *bytes);
  *   bias   fp32           bias[b*strideBias + j], NULLABLE
  *   out    typeO          out[b*strideO + i*ldo + j]   (written; K = 0 gives the bias, or 0)
  *   workspace             as sc_gemm's; NULL where sc_fp8_gemm_workspace_size gives 0
- * The order of the sums depends on the sizes alone: same call, same bits.
+ * The order of the sums depends on sizes, types, strides and alignment alone: same call, same bits.
  */
 int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, const void *B, const float *sB,
                 const float *bias, void *out, void *workspace, size_t workspace_bytes, void *stream);
@@ -361,7 +361,7 @@ int sc_residual_norm_backward_workspace_size(const sc_norm_desc *desc, size_t *b
  *   dpost_w, dpost_b, dgate, dpre_w, dpre_b   fp32, NULLABLE (written): the parameter's gradient, [b*D + d], or
  *             [d] summed over the batch too where the parameter's batch stride is 0
  * xo may be NULL where pre is SC_NORM_NONE and neither dpre_w nor dpre_b is wanted; y where post is SC_NORM_NONE and
- * neither dgate nor a post gradient is wanted.  The sums' order depends on the sizes alone: same call, same bits.
+ * neither dgate nor a post gradient is wanted.  The order of the sums depends on sizes, types, strides and alignment alone: same call, same bits.
  */
 int sc_residual_norm_backward(const sc_norm_desc *desc, const void *xo, const void *y, const void *post_w,
                               const void *post_b, const void *gate, const void *pre_w, const void *dxo,

@@ -7,8 +7,8 @@
 namespace scl {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
-typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
 // ----------------------------------------------------------------------------
 // quantiser
@@ -240,7 +240,7 @@ struct GemmArgs {
     void *out;
     int64_t lda, ldb, ldo, strideA, strideB, strideO, ldsA, ldsB, strideSA, strideSB, strideBias;
     int shiftA, shiftB;          // log2 of the rows that share a scale
-    int typeO, vecO;             // vecO: four outputs of a row can be stored at once
+    int typeO, whole;            // whole: output rows of whole 16-byte stores, at 32-bit offsets in a tile
     int tilesM, tilesN, batch;
 };
 
@@ -250,7 +250,7 @@ struct GemmArgs {
 // The matrix cores' 8-bit products keep, of each eight neighbours in a lane, what lies within 2^-13 of the
 // largest one's power of two (measured: beside a product of 2^16 one of 2^3 counts and one of 2^2 does not) and add the
 // eights in float32.  That is far inside the rounding of a 16-bit result.  EXACT, for float32 results, turns the
-// bytes into bfloat16 (every value of both types is one) and takes the 16-bit products, whose sums are float32
+// bytes into float16 (every value of both types is one) and takes the 16-bit products, whose sums are float32
 // throughout, at half the rate.
 template <int T, bool EXACT>
 struct Frag {
@@ -261,17 +261,18 @@ struct Frag {
 };
 template <int T>
 struct Frag<T, true> {
-    b8 w[4];
-    __device__ __forceinline__ b2 pair(uint32_t x, bool upper) {
-        if (T == 0) return upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false);
-        return upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(x, 1.0f, false);
+    h8 w[4];
+    // e5m2 is float16's upper byte; e4m3 is converted, two at a time
+    static __device__ __forceinline__ h2 pair(uint32_t x, bool upper) {
+        if (T == 1) return __builtin_bit_cast(h2, __builtin_amdgcn_perm(x, 0u, upper ? 0x070c060cu : 0x050c040cu));
+        return upper ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false);
     }
     __device__ __forceinline__ void set(u4 lo, u4 hi) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t x = k < 2 ? lo[2 * k] : hi[2 * k - 4], y = k < 2 ? lo[2 * k + 1] : hi[2 * k - 3];
-            const b2 p = pair(x, false), q = pair(x, true), r = pair(y, false), s = pair(y, true);
-            w[k] = b8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+            const h2 p = pair(x, false), q = pair(x, true), r = pair(y, false), s = pair(y, true);
+            w[k] = h8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
         }
     }
 };
@@ -283,7 +284,7 @@ template <int TX, int TY>
 __device__ __forceinline__ f4 mma_128(const Frag<TX, true> &x, const Frag<TY, true> &y) {
     f4 d = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.w[k], y.w[k], d, 0, 0, 0);
+    for (int k = 0; k < 4; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x.w[k], y.w[k], d, 0, 0, 0);
     return d;
 }
 
@@ -291,21 +292,28 @@ __device__ __forceinline__ f4 mma_128(const Frag<TX, true> &x, const Frag<TY, tr
 __device__ __forceinline__ u4 load_granule(const uint8_t *row, int k, int K) {
     if (k + 16 <= K) return *reinterpret_cast<const u4_any *>(row + k);
     u4 w = {0u, 0u, 0u, 0u};
+    if (k >= K) return w;
+    if (K >= 16) {
+        // the row's last sixteen, moved down over those that lie before k
+        const u4 x = *reinterpret_cast<const u4_any *>(row + K - 16);
+        const uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
+        const int s = 8 * (k + 16 - K);              // 8 .. 120 bits
+        const uint64_t l = s >= 64 ? hi >> (s - 64) : lo >> s | hi << (64 - s), h = s >= 64 ? 0u : hi >> s;
+        return u4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+    }
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (k + j < K) w[j >> 2] |= (uint32_t)row[k + j] << (8 * (j & 3));
+    for (int j = 0; j < 15; ++j)                     // (k is 0)
+        if (j < K) w[j >> 2] |= (uint32_t)row[j] << (8 * (j & 3));
     return w;
-}
-
-__device__ __forceinline__ void store_out4(const GemmArgs &g, int b, int64_t i, int j, f4 v) {
-    const int64_t at = (int64_t)b * g.strideO + i * g.ldo + j;
-    if (g.vecO && j + 4 <= g.N) store4<true>(g.typeO, g.out, at, v, 4);
-    else store4<false>(g.typeO, g.out, at, v, g.N - j);
 }
 
 // LDS holds a stage of 128 elements as rows of eight 16-byte granules; granule q of row r lies at
 // q ^ swz(r), so that the 16 rows that a fragment read takes at one granule spread over all banks
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
+// The rows of B go to the matrix cores in an order that gives a lane neighbouring columns: row 4 q + e of fragment j is
+// row 16 q + 4 j + e of 64, so its sums over the four fragments are 16 columns in a row.  Their granules' places:
+__device__ __forceinline__ int fragment_row(int l16, int j) { return 16 * (l16 >> 2) + 4 * j + (l16 & 3); }
+__device__ __forceinline__ int swz_b(int r) { return ((r >> 1) & 1) | ((r >> 3) & 6); }
 
 // Copies 16 (or 4) bytes for each lane from the buffer, at off, to LDS, at `to` (the same in every lane) plus 16 (4)
 // bytes a lane, past the registers.  Nothing waits for it but wait_copies().  What lies behind the buffer's bound
@@ -350,152 +358,81 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t tiles, int tilesM,
     *tn = (int)(in / rows);
 }
 
-// A tile of BM x BN outputs by waves of WM x WN each.  A scale block is one stage: the matrix cores sum its
-// 128 products from zero and the sum enters the accumulators times its two scales.
-template <int TA, int TB, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_any(GemmArgs g) {
-    constexpr int NT = (BM / WM) * (BN / WN) * 64, MI = WM / 16, NI = WN / 16, GA = BM * 8 / NT, GB = BN * 8 / NT;
-    __shared__ u4 sm[(BM + BN) * 8];
-    __shared__ float sc[BM + BN];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, q4 = lane >> 4;
-    const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
-    const int64_t m0 = (int64_t)(block_id() % (uint32_t)g.tilesM) * BM, n0 = (int64_t)(block_id() / (uint32_t)g.tilesM) * BN;
-    if (n0 >= g.N) return;
-    for (int b = blockIdx.z; b < g.batch; b += gridDim.z) {
-        const uint8_t *A = g.A + (int64_t)b * g.strideA, *B = g.B + (int64_t)b * g.strideB;
-        const float *sA = g.sA + (int64_t)b * g.strideSA, *sB = g.sB + (int64_t)b * g.strideSB;
-        f4 acc[MI][NI];
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int t = 0; t < g.KB; ++t) {
-            u4 ra[GA], rb[GB];
-#pragma unroll
-            for (int k = 0; k < GA; ++k) {
-                const int x = tid + k * NT;
-                ra[k] = load_granule(A + min(m0 + (x >> 3), (int64_t)g.M - 1) * g.lda, t * 128 + 16 * (x & 7), g.K);
-            }
-#pragma unroll
-            for (int k = 0; k < GB; ++k) {
-                const int x = tid + k * NT;
-                rb[k] = load_granule(B + min(n0 + (x >> 3), (int64_t)g.N - 1) * g.ldb, t * 128 + 16 * (x & 7), g.K);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < GA; ++k) {
-                const int x = tid + k * NT, r = x >> 3;
-                sm[r * 8 + ((x & 7) ^ swz(r))] = ra[k];
-            }
-#pragma unroll
-            for (int k = 0; k < GB; ++k) {
-                const int x = tid + k * NT, r = x >> 3;
-                sm[(BM + r) * 8 + ((x & 7) ^ swz(r))] = rb[k];
-            }
-            for (int x = tid; x < BM + BN; x += NT)
-                sc[x] = x < BM ? sA[(min(m0 + x, (int64_t)g.M - 1) >> g.shiftA) * g.ldsA + t]
-                               : sB[(min(n0 + x - BM, (int64_t)g.N - 1) >> g.shiftB) * g.ldsB + t];
-            __syncthreads();
-            Frag<TB, EXACT> fb[NI];
-            f4 sb[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int r = wn + 16 * j + l16;
-                const u4 lo = sm[(BM + r) * 8 + ((2 * q4) ^ swz(r))], hi = sm[(BM + r) * 8 + ((2 * q4 + 1) ^ swz(r))];
-                fb[j].set(lo, hi);
-                sb[j] = *reinterpret_cast<const f4 *>(&sc[BM + wn + 16 * j + 4 * q4]);
-            }
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int r = wm + 16 * i + l16;
-                const u4 lo = sm[r * 8 + ((2 * q4) ^ swz(r))], hi = sm[r * 8 + ((2 * q4 + 1) ^ swz(r))];
-                Frag<TA, EXACT> fa;
-                fa.set(lo, hi);
-                const float s = sc[r];
-#pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    const f4 p = mma_128(fb[j], fa);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] += p[e] * (s * sb[j][e]);
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int64_t m = m0 + wm + 16 * i + l16;
-            if (m >= g.M) continue;
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int64_t n = n0 + wn + 16 * j + 4 * q4;
-                if (n >= g.N) continue;
-                f4 v = acc[i][j];
-                if (g.bias) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n + e < g.N) v[e] += g.bias[(int64_t)b * g.strideBias + n + e];
-                }
-                store_out4(g, b, m, (int)n, v);
-            }
-        }
-    }
-}
-
-// A wave's outputs from row m0 and column n0 on: lane (q4, l16) holds rows 16 i + l16, columns 16 j + 4 q4 .. + 3.
-// Stores carry 32-bit offsets from the corner; rows behind the last lie behind the buffer's bound, which drops them, and
-// columns behind the last are sent there, so nothing branches.  (store_tile's caller has 16 MI rows in 2^30 bytes.)
-template <int TO, bool QUADS, int MI, int NI>
-__device__ __forceinline__ void store_rows(const __amdgpu_buffer_rsrc_t o, const float *bias, int cols, uint32_t ldo, int l16, int q4,
+// A wave's outputs from row m0 and column n0 on: lane (q4, l16) holds rows 16 i + l16 and, in fragment j, columns 16 j + 4 q4 .. + 3;
+// RUN: 16 q4 + 4 j .. + 3 (fragment_row), so that two fragments' 16-bit outputs are stored together.
+// WHOLE: rows of whole 16-byte stores.  Stores then carry 32-bit offsets from the corner; rows behind the last lie
+// behind the buffer's bound, which drops them, and columns behind the last are sent there, so nothing branches
+// (16 MI rows lie in 2^30 bytes).  Otherwise stores go by address, of any alignment, and a run that is cut by the row's end goes
+// element by element.
+template <int TO, bool WHOLE, bool RUN, int MI, int NI>
+__device__ __forceinline__ void store_rows(uint8_t *corner, const float *bias, int rows, int cols, int64_t ldo, int l16, int q4,
                                            const f4 (&acc)[MI][NI]) {
-    constexpr uint32_t ES = TO == SC_F32 ? 4 : 2, BEHIND = 0x80000000u;
-    const uint32_t row = (uint32_t)l16 * ldo * ES, step = 16u * ldo * ES;
+    constexpr int ES = TO == SC_F32 ? 4 : 2, STEP = RUN && TO != SC_F32 ? 2 : 1;   // fragments that are stored together
+    constexpr uint32_t BEHIND = 0x80000000u;
+    const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(corner, 0, (int)(((rows - 1) * ldo + cols) * ES), 0x00020000);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-        const int n = 16 * j + 4 * q4;
-        f4 add = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (bias)
+    for (int j = 0; j < NI; j += STEP) {
+        const int n = RUN ? 16 * q4 + 4 * j : 16 * j + 4 * q4;
+        f4 add[STEP];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add[e] = bias[min(n + e, cols - 1)];
-        uint32_t at[4];
+        for (int h = 0; h < STEP; ++h) {
+            add[h] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (bias)
 #pragma unroll
-        for (int e = 0; e < (QUADS ? 1 : 4); ++e) at[e] = n + e < cols ? row + (uint32_t)(n + e) * ES : BEHIND;
+                for (int e = 0; e < 4; ++e) add[h][e] = bias[min(n + 4 * h + e, cols - 1)];
+        }
+        const uint32_t at = n < cols ? (l16 * (uint32_t)ldo + n) * ES : BEHIND;
+        uint8_t *p = corner + (l16 * ldo + n) * ES;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const f4 v = acc[i][j] + add;
-            if (QUADS && TO == SC_F32) {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), o, at[0] + i * step, 0, 0);
-            } else if (QUADS) {
-                uint32_t h[4];
+        for (int i = 0; i < MI; ++i, p += 16 * ldo * ES) {
+            if (!WHOLE) __builtin_amdgcn_sched_barrier(0);       // (one row's addresses at a time)
+            uint32_t w[TO == SC_F32 ? 4 : 2 * STEP];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e]);
-                __builtin_amdgcn_raw_buffer_store_b64(u2{h[0] | h[1] << 16, h[2] | h[3] << 16}, o, at[0] + i * step, 0, 0);
-            } else {
+            for (int h = 0; h < STEP; ++h) {
+                const f4 v = acc[i][j + h] + add[h];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (TO == SC_F32) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), o, at[e] + i * step, 0, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e])), o, at[e] + i * step, 0, 0);
+                    if (TO == SC_F32) w[e] = __float_as_uint(v[e]);
+                    else if (e & 1) w[2 * h + (e >> 1)] |= (TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e])) << 16;
+                    else w[2 * h + (e >> 1)] = TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e]);
+                }
+            }
+            constexpr int WORDS = TO == SC_F32 ? 4 : 2 * STEP;
+            if (WHOLE) {
+                const uint32_t to = at + (uint32_t)i * 16u * (uint32_t)ldo * ES;
+                if (WORDS == 4) __builtin_amdgcn_raw_buffer_store_b128(u4{w[0], w[1], w[WORDS - 2], w[WORDS - 1]}, o, to, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b64(u2{w[0], w[1]}, o, to, 0, 0);
+            } else if (16 * i + l16 < rows && n < cols) {
+                if (n + 4 * STEP <= cols) {
+                    if (WORDS == 4) *reinterpret_cast<u4_any *>(p) = u4{w[0], w[1], w[WORDS - 2], w[WORDS - 1]};
+                    else *reinterpret_cast<u2_any *>(p) = u2{w[0], w[1]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4 * STEP; ++e) {
+                        if (n + e >= cols) continue;
+                        if (TO == SC_F32) reinterpret_cast<uint32_t *>(p)[e] = w[e & 3];
+                        else reinterpret_cast<uint16_t *>(p)[e] = (uint16_t)(w[(e >> 1) % WORDS] >> (16 * (e & 1)));
+                    }
                 }
             }
         }
     }
 }
-template <bool EXACT, int MI, int NI>
+template <bool EXACT, bool RUN, int MI, int NI>
 __device__ __forceinline__ void store_tile(const GemmArgs &g, int b, int64_t m0, int64_t n0, int l16, int q4, const f4 (&acc)[MI][NI]) {
-    const int64_t es = EXACT ? 4 : 2;
     const int rows = (int)min(g.M - m0, (int64_t)(16 * MI)), cols = (int)min(g.N - n0, (int64_t)(16 * NI));
     if (rows <= 0 || cols <= 0) return;
-    uint8_t *corner = static_cast<uint8_t *>(g.out) + (b * g.strideO + m0 * g.ldo + n0) * es;
-    const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(corner, 0, (int)(((rows - 1) * g.ldo + cols) * es), 0x00020000);
+    uint8_t *corner = static_cast<uint8_t *>(g.out) + (b * g.strideO + m0 * g.ldo + n0) * (EXACT ? 4 : 2);
     const float *bias = g.bias ? g.bias + b * g.strideBias + n0 : nullptr;
-    const uint32_t ldo = (uint32_t)g.ldo;
     if (EXACT) {
-        if (g.vecO) store_rows<SC_F32, true>(o, bias, cols, ldo, l16, q4, acc);
-        else store_rows<SC_F32, false>(o, bias, cols, ldo, l16, q4, acc);
+        if (g.whole) store_rows<SC_F32, true, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
+        else store_rows<SC_F32, false, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
     } else if (g.typeO == SC_BF16) {
-        if (g.vecO) store_rows<SC_BF16, true>(o, bias, cols, ldo, l16, q4, acc);
-        else store_rows<SC_BF16, false>(o, bias, cols, ldo, l16, q4, acc);
+        if (g.whole) store_rows<SC_BF16, true, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
+        else store_rows<SC_BF16, false, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
     } else {
-        if (g.vecO) store_rows<SC_F16, true>(o, bias, cols, ldo, l16, q4, acc);
-        else store_rows<SC_F16, false>(o, bias, cols, ldo, l16, q4, acc);
+        if (g.whole) store_rows<SC_F16, true, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
+        else store_rows<SC_F16, false, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
     }
 }
 
@@ -504,10 +441,12 @@ __device__ __forceinline__ void store_tile(const GemmArgs &g, int b, int64_t m0,
 // scales.  A stage's operands and scales are copied to LDS while the stage before it is multiplied.
 // BLOCKB: the rows of B share a scale by 128, so a wave's columns have one.
 template <int TA, int TB, bool EXACT, bool BLOCKB, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArgs g, uint32_t tiles) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(GemmArgs g, uint32_t tiles) {
     constexpr int NW = (BM / WM) * (BN / WN), MI = WM / 16, NI = WN / 16, ROWS = BM + BN;
     constexpr int WR = ROWS / NW, CH = WR / 8;      // rows that a wave copies of each stage, eight at a time
-    static_assert(WR == 64 && BM % WR == 0, "a wave copies rows of one operand, and a scale for each of its lanes");
+    constexpr bool ALONE = BM == 256;               // a block to a compute unit
+    constexpr int EARLY = ALONE ? 4 : 1;            // a stage is sent for during the first 1 / EARLY of the row groups
+    static_assert(NI == 4 && WR == 64 && BM % WR == 0, "a wave copies rows of one operand, and a scale for each of its lanes");
     __shared__ u4 sm[2][ROWS * 8];
     __shared__ float sc[2][ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q4 = lane >> 4;
@@ -524,7 +463,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArg
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int r = r0 + 8 * k + (lane >> 3);
-        off[k] = (uint32_t)r * (uint32_t)ld + 16u * ((lane & 7) ^ swz(r));
+        off[k] = (uint32_t)r * (uint32_t)ld + 16u * ((lane & 7) ^ (forB ? swz_b(r) : swz(r)));
     }
     const uint32_t soff = 4u * (uint32_t)((r0 + lane) >> shift) * (uint32_t)lds;
     // the next stage to copy: stage ct of the tile (cb, cm, cn)
@@ -573,29 +512,30 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArg
 #pragma unroll 1
                 for (int k = 0; k < CH; ++k) {
                     u4 *p = &sm[buf][(wave * CH + k) * 64 + lane];
-                    const int left = cut - 16 * ((lane & 7) ^ swz(8 * k + (lane >> 3)));
+                    const int r = r0 + 8 * k + (lane >> 3), left = cut - 16 * ((lane & 7) ^ (forB ? swz_b(r) : swz(r)));
                     *p &= u4{bytes_before(left), bytes_before(left - 4), bytes_before(left - 8), bytes_before(left - 12)};
                 }
             }
             __syncthreads();          // everyone's copies have arrived, and the other buffer has been read
             advance();
             // Row group i is multiplied while group i + 1 is read, a part of the next stage is sent for and the sums of group
-            // i - 1 are scaled.  The fences hold that order: left to itself the compiler scales a group's sums as soon as they
-            // are there, and both waves of a SIMD then wait for the same unit in turn.
+            // i - 1 are scaled.  The fences hold that order (one a row group where two blocks share a compute unit and fill each
+            // other's gaps): left to itself the compiler would draw the reads together, into more registers than there are.
             const u4 *s = sm[buf];
-            const auto read = [&](auto &f, int r) { f.set(s[r * 8 + (q4 ^ swz(r))], s[r * 8 + ((q4 + 4) ^ swz(r))]); };
             Frag<TB, EXACT> fb[NI];
             Frag<TA, EXACT> fa[2];
             f4 sb[BLOCKB ? 1 : NI], p[2][NI];
             float sa[3];
-            read(fa[0], wm + l16);
+            const auto read = [&](auto &f, int r, int z) { f.set(s[r * 8 + (q4 ^ z)], s[r * 8 + ((q4 + 4) ^ z)]); };
+            const auto read_a = [&](int i) { read(fa[i & 1], wm + 16 * i + l16, swz(l16)); };
+            read_a(0);
 #pragma unroll
-            for (int j = 0; j < NI; ++j) read(fb[j], BM + wn + 16 * j + l16);
+            for (int j = 0; j < NI; ++j) read(fb[j], BM + wn + fragment_row(l16, j), swz_b(fragment_row(l16, j)));
             if (BLOCKB) {
                 sb[0] = f4{sc[buf][BM + wn], 0.0f, 0.0f, 0.0f};
             } else {
 #pragma unroll
-                for (int j = 0; j < NI; ++j) sb[j] = *reinterpret_cast<const f4 *>(&sc[buf][BM + wn + 16 * j + 4 * q4]);
+                for (int j = 0; j < NI; ++j) sb[j] = *reinterpret_cast<const f4 *>(&sc[buf][BM + wn + 16 * q4 + 4 * j]);
             }
             sa[0] = sc[buf][wm + l16];
             copy_scales(buf ^ 1);
@@ -607,60 +547,351 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_fp8_gemm(GemmArg
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 if (i + 1 < MI) {
-                    read(fa[(i + 1) & 1], wm + 16 * (i + 1) + l16);
+                    read_a(i + 1);
                     sa[(i + 1) % 3] = sc[buf][wm + 16 * (i + 1) + l16];
                 }
 #pragma unroll
-                for (int k = i * CH / MI; k < (i + 1) * CH / MI; ++k) copy(buf ^ 1, k);
+                for (int k = i * CH / MI * EARLY; k < (i + 1) * CH / MI * EARLY; ++k)
+                    if (k < CH) copy(buf ^ 1, k);
 #pragma unroll
                 for (int j = 0; j < NI; ++j) {
                     p[i & 1][j] = mma_128(fb[j], fa[i & 1]);
-                    if (i > 0) add(i - 1, j);
-                    __builtin_amdgcn_sched_barrier(0);
+                    if (ALONE && i > 0) add(i - 1, j);
+                    if (ALONE) __builtin_amdgcn_sched_barrier(0);
                 }
                 if (BLOCKB) sa[i % 3] *= sb[0][0];
-            }
+                if (!ALONE) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j) add(MI - 1, j);
+                    for (int j = 0; j < NI; ++j) add(i, j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (ALONE)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) add(MI - 1, j);
             buf ^= 1;
         }
         if (g.KB == 0) {
             next += gridDim.x;
             if (next < tiles) enter();
         }
-        store_tile<EXACT, MI, NI>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+        store_tile<EXACT, true>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+    }
+}
+
+// Few rows, few tiles, or operands off 16 bytes: a block has 16 MI x 16 NI outputs, and its eight waves deal the
+// blocks of 128 among themselves.  A wave takes its fragments from memory as they lie (a row's 128 bytes by four lanes, 64 of
+// them at a time), the next block's while one is multiplied; the eight sums are joined in LDS in order.
+constexpr int DW = 8;
+template <int TA, int TB, bool EXACT, int MI, int NI>
+__global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t tiles) {
+    __shared__ f4 join[DW][MI * NI][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
+    if (block_id() >= tiles) return;
+    const int64_t m0 = (int64_t)(block_id() % (uint32_t)g.tilesM) * (16 * MI), n0 = (int64_t)(block_id() / (uint32_t)g.tilesM) * (16 * NI);
+    for (int b = blockIdx.z; b < g.batch; b += gridDim.z) {
+        const uint8_t *A = g.A + b * g.strideA, *B = g.B + b * g.strideB;
+        const float *sA = g.sA + b * g.strideSA, *sB = g.sB + b * g.strideSB;
+        // (rows behind the last read the last one; their outputs are not stored)
+        uint32_t ra[MI], rb[NI], sb[NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) ra[i] = (uint32_t)min(m0 + 16 * i + l16, (int64_t)g.M - 1);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            rb[j] = (uint32_t)min(n0 + 16 * j + l16, (int64_t)g.N - 1);
+            sb[j] = (uint32_t)min(n0 + 16 * j + 4 * q4, (int64_t)g.N - 1);
+        }
+        f4 acc[MI][NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        struct Block {
+            u4 a[MI][2], b[NI][2];
+            float sa[MI];
+            f4 sb[NI];
+        };
+        const auto fetch = [&](Block &f, int t) {
+            const int k = 128 * t + 16 * q4;
+            if (128 * t + 128 <= g.K) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) f.a[i][h] = *reinterpret_cast<const u4_any *>(A + ra[i] * g.lda + k + 64 * h);
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) f.b[j][h] = *reinterpret_cast<const u4_any *>(B + rb[j] * g.ldb + k + 64 * h);
+            } else {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) f.a[i][h] = load_granule(A + ra[i] * g.lda, k + 64 * h, g.K);
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) f.b[j][h] = load_granule(B + rb[j] * g.ldb, k + 64 * h, g.K);
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) f.sa[i] = sA[(ra[i] >> g.shiftA) * g.ldsA + t];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                if (g.shiftB) {
+                    const float s = sB[(sb[j] >> 7) * g.ldsB + t];
+                    f.sb[j] = f4{s, s, s, s};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f.sb[j][e] = sB[min(sb[j] + e, (uint32_t)g.N - 1u) * g.ldsB + t];
+                }
+            }
+        };
+        const auto multiply = [&](const Block &f) {
+            Frag<TB, EXACT> fb[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) fb[j].set(f.b[j][0], f.b[j][1]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                Frag<TA, EXACT> fa;
+                fa.set(f.a[i][0], f.a[i][1]);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const f4 p = mma_128(fb[j], fa);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], f.sa[i] * f.sb[j][e], acc[i][j][e]);
+                }
+            }
+        };
+        Block now, then;
+        if (wave < g.KB) fetch(now, wave);
+        for (int t = wave; t < g.KB; t += DW) {
+            if (t + DW < g.KB) fetch(then, t + DW);
+            multiply(now);
+            now = then;
+        }
+        __syncthreads();                 // (the last batch entry's sums have been read)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) join[wave][i * NI + j][lane] = acc[i][j];
+        __syncthreads();
+        for (int x = wave; x < MI * NI; x += DW) {
+            f4 v[1][1] = {{join[0][x][lane]}};
+#pragma unroll
+            for (int w = 1; w < DW; ++w) v[0][0] += join[w][x][lane];
+            store_tile<EXACT, false>(g, b, m0 + 16 * (x / NI), n0 + 16 * (x % NI), l16, q4, v);
+        }
+    }
+}
+
+// Too few tiles for every compute unit, or operands off 16 bytes: a block has 64 x 64 outputs, and KG groups of four waves
+// take every KG-th block of 128 each, through registers (which take any alignment) into two stages of LDS of their own, the
+// next block's loads in flight while one is multiplied; the groups' sums are joined in LDS in order.
+template <int TA, int TB, bool EXACT, int KG>
+__global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t tiles) {
+    constexpr int T = 64, G = 2 * T * 8 / 256;       // granules a thread
+    __shared__ u4 sm[KG][2][2 * T * 8];
+    __shared__ float sc[KG][2][2 * T];
+    const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6,
+              l16 = lane & 15, q4 = lane >> 4, wm = 32 * (wave & 1), wn = 32 * (wave >> 1);
+    if (block_id() >= tiles) return;
+    const int64_t m0 = (int64_t)(block_id() % (uint32_t)g.tilesM) * T, n0 = (int64_t)(block_id() / (uint32_t)g.tilesM) * T;
+    for (int b = blockIdx.z; b < g.batch; b += gridDim.z) {
+        const uint8_t *row[G];
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            const int r = (k * 256 + tid) >> 3;      // (rows behind the last read the last one; their outputs are not stored)
+            row[k] = k < G / 2 ? g.A + b * g.strideA + min(m0 + r, (int64_t)g.M - 1) * g.lda
+                               : g.B + b * g.strideB + min(n0 + r - T, (int64_t)g.N - 1) * g.ldb;
+        }
+        const float *scale = tid < T ? g.sA + b * g.strideSA + (min(m0 + tid, (int64_t)g.M - 1) >> g.shiftA) * g.ldsA
+                                     : g.sB + b * g.strideSB + (min(n0 + (tid & (T - 1)), (int64_t)g.N - 1) >> g.shiftB) * g.ldsB;
+        f4 acc[2][2] = {};
+        u4 r[G];
+        float s = 0.0f;
+        const auto load = [&](int t) {
+#pragma unroll
+            for (int k = 0; k < G; ++k) r[k] = load_granule(row[k], 128 * t + 16 * (tid & 7), g.K);
+            if (tid < 2 * T) s = scale[t];
+        };
+        const auto put = [&](int buf) {
+#pragma unroll
+            for (int k = 0; k < G; ++k) {
+                const int x = (k * 256 + tid) >> 3;
+                sm[grp][buf][x * 8 + ((tid & 7) ^ swz(x))] = r[k];
+            }
+            if (tid < 2 * T) sc[grp][buf][tid] = s;
+        };
+        __syncthreads();                             // (the last batch entry's sums have been read)
+        if (grp < g.KB) {
+            load(grp);
+            put(0);
+        }
+        int buf = 0;
+        for (int t = grp; t - grp < g.KB; t += KG, buf ^= 1) {
+            __syncthreads();
+            const bool more = t + KG < g.KB;
+            if (more) load(t + KG);
+            if (t < g.KB) {
+                const u4 *p = sm[grp][buf];
+                const auto read = [&](auto &f, int x) { f.set(p[x * 8 + (q4 ^ swz(x))], p[x * 8 + ((q4 + 4) ^ swz(x))]); };
+                Frag<TB, EXACT> fb[2];
+                f4 sb[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    read(fb[j], T + wn + 16 * j + l16);
+                    sb[j] = *reinterpret_cast<const f4 *>(&sc[grp][buf][T + wn + 16 * j + 4 * q4]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Frag<TA, EXACT> fa;
+                    read(fa, wm + 16 * i + l16);
+                    const float sa = sc[grp][buf][wm + 16 * i + l16];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const f4 d = mma_128(fb[j], fa);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(d[e], sa * sb[j][e], acc[i][j][e]);
+                    }
+                }
+            }
+            if (more) put(buf ^ 1);
+        }
+        if (KG > 1) {
+            f4 *join = reinterpret_cast<f4 *>(sm);   // [KG - 1][4][256]
+            __syncthreads();
+            if (grp > 0)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) join[((grp - 1) * 4 + x) * 256 + tid] = acc[x >> 1][x & 1];
+            __syncthreads();
+            if (grp > 0) continue;
+#pragma unroll
+            for (int w = 0; w < KG - 1; ++w)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) acc[x >> 1][x & 1] += join[(w * 4 + x) * 256 + tid];
+        }
+        store_tile<EXACT, false>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
     }
 }
 
 template <int TA, int TB, bool EXACT, bool BLOCKB, int BM, int BN, int WM, int WN>
-static hipError_t launch_tile(const GemmArgs &g0, int per_cu, hipStream_t st) {
-    GemmArgs g = g0;
+static void launch_tile(GemmArgs g, int per_cu, hipStream_t st) {
     g.tilesM = (int)(((int64_t)g.M + BM - 1) / BM);
     g.tilesN = (int)(((int64_t)g.N + BN - 1) / BN);
     const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN * (uint32_t)g.batch, most = 256u * per_cu;
     hipLaunchKernelGGL((k_fp8_gemm<TA, TB, EXACT, BLOCKB, BM, BN, WM, WN>), dim3(tiles < most ? tiles : most), dim3((BM / WM) * (BN / WN) * 64),
                        0, st, g, tiles);
-    return hipGetLastError();
 }
-template <int TA, int TB, bool EXACT>
-static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
-    const bool al = aligned_to(g.A, 16) && aligned_to(g.B, 16) && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.strideA % 16 == 0 && g.strideB % 16 == 0;
-    if (!al || g.lda > (1 << 23) || g.ldb > (1 << 23) || g.ldsA > (1 << 21) || g.ldsB > (1 << 21) || g.ldo > (1 << 20) || getenv("SCT0")) {
-        GemmArgs h = g;
-        h.tilesM = (int)(((int64_t)g.M + 127) / 128);
-        h.tilesN = (int)(((int64_t)g.N + 127) / 128);
-        hipLaunchKernelGGL((k_fp8_any<TA, TB, EXACT, 128, 128, 64, 64>), grid_of((uint32_t)h.tilesM * (uint32_t)h.tilesN, g.batch), dim3(256), 0, st, h);
-        return hipGetLastError();
-    }
-    if (getenv("SCT") && atoi(getenv("SCT")) == 1) return g.shiftB ? launch_tile<TA, TB, EXACT, true, 128, 128, 64, 64>(g, 2, st) : launch_tile<TA, TB, EXACT, false, 128, 128, 64, 64>(g, 2, st);
-    if (EXACT) return g.shiftB ? launch_tile<TA, TB, EXACT, true, 128, 128, 64, 64>(g, 2, st) : launch_tile<TA, TB, EXACT, false, 128, 128, 64, 64>(g, 2, st);
-    return g.shiftB ? launch_tile<TA, TB, false, true, 256, 256, 128, 64>(g, 1, st) : launch_tile<TA, TB, false, false, 256, 256, 128, 64>(g, 1, st);
+template <int TA, int TB, bool EXACT, int MI, int NI>
+static void launch_direct(GemmArgs g, hipStream_t st) {
+    g.tilesM = (int)(((int64_t)g.M + 16 * MI - 1) / (16 * MI));
+    g.tilesN = (int)(((int64_t)g.N + 16 * NI - 1) / (16 * NI));
+    const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN;
+    hipLaunchKernelGGL((k_fp8_direct<TA, TB, EXACT, MI, NI>), grid_of(tiles, g.batch), dim3(64 * DW), 0, st, g, tiles);
+}
+template <int TA, int TB, bool EXACT, int KG>
+static void launch_parts(GemmArgs g, hipStream_t st) {
+    g.tilesM = (int)(((int64_t)g.M + 63) / 64);
+    g.tilesN = (int)(((int64_t)g.N + 63) / 64);
+    const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN;
+    hipLaunchKernelGGL((k_fp8_parts<TA, TB, EXACT, KG>), grid_of(tiles, g.batch), dim3(256 * KG), 0, st, g, tiles);
+}
+// An operand whose rows do not start on 16 bytes, laid out anew: rows of whole blocks of 128, zeros behind K.  Memory-bound,
+// and worth it where many tiles read every row.
+__global__ __launch_bounds__(256) void k_fp8_lay(const uint8_t *src, int64_t ld, int64_t stride, int rows, int K, int KB, int batch,
+                                                 uint8_t *dst) {
+    const int64_t each = (int64_t)rows * KB * 8, all = each * batch, at = (int64_t)block_id() * 256 + threadIdx.x;
+    if (at >= all) return;
+    const int64_t b = at / each, in = at - b * each, row = in / (KB * 8);
+    const int q = (int)(in - row * (KB * 8));
+    reinterpret_cast<u4 *>(dst)[at] = load_granule(src + b * stride + row * ld, 16 * q, K);
 }
 
+// How a product is done.  Tiles of 128 x 128 (two blocks to a compute unit) or, for 16-bit results, 256 x 256 (one) where there
+// are enough for half of the compute units; their operands have to lie on 16 bytes, or are laid out so first.  Few tiles:
+// 64 x 64 by groups of waves.  Up to 16 rows: without LDS.
+enum { DIRECT, PARTS, TILES };
+static int64_t tiles_of(const GemmArgs &g, int side) { return ((int64_t)g.M + side - 1) / side * (((int64_t)g.N + side - 1) / side) * g.batch; }
+static bool rows_aligned(int64_t ld, int64_t stride, int batch) { return ld % 16 == 0 && (batch == 1 || stride % 16 == 0); }
+static int way_of(const GemmArgs &g) {
+    if (g.M <= 16 || g.KB == 0) return DIRECT;
+    const int64_t tiles = tiles_of(g, 128);
+    // (copies to LDS and a tile's scales have 32-bit offsets)
+    return tiles < 128 || tiles > INT32_MAX / 4 || g.ldsA > 1 << 21 || g.ldsB > 1 << 21 ? PARTS : TILES;
+}
+static size_t laid_bytes(int rows, int KB, int64_t stride, int batch) {
+    return (size_t)rows * KB * 128 * (stride == 0 ? 1 : batch);
+}
+// bytes that the operands take that have to be laid out, A's first
+static void lay_sizes(const GemmArgs &g, size_t *a, size_t *b) {
+    const bool tiles = way_of(g) == TILES;
+    *a = tiles && (!rows_aligned(g.lda, g.strideA, g.batch) || g.lda > 1 << 22) ? laid_bytes(g.M, g.KB, g.strideA, g.batch) : 0;
+    *b = tiles && (!rows_aligned(g.ldb, g.strideB, g.batch) || g.ldb > 1 << 22) ? laid_bytes(g.N, g.KB, g.strideB, g.batch) : 0;
+    *a = (*a + 255) / 256 * 256;
+}
+static hipError_t lay(const uint8_t **p, int64_t *ld, int64_t *stride, int rows, const GemmArgs &g, uint8_t *dst, hipStream_t st) {
+    const int batch = *stride == 0 ? 1 : g.batch;
+    const int64_t granules = (int64_t)rows * g.KB * 8 * batch;
+    hipLaunchKernelGGL(k_fp8_lay, grid_of((uint32_t)((granules + 255) / 256), 1), dim3(256), 0, st, *p, *ld, *stride, rows, g.K, g.KB, batch, dst);
+    *p = dst;
+    *ld = (int64_t)g.KB * 128;
+    *stride = *stride == 0 ? 0 : (int64_t)rows * g.KB * 128;
+    return hipGetLastError();
+}
+
+template <int TA, int TB, bool EXACT>
+static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
+    const bool tiled = way_of(g) == TILES && aligned_to(g.A, 16) && aligned_to(g.B, 16) && rows_aligned(g.lda, g.strideA, g.batch) &&
+                       rows_aligned(g.ldb, g.strideB, g.batch);
+    if (way_of(g) == DIRECT) {
+        launch_direct<TA, TB, EXACT, 1, 1>(g, st);
+    } else if (!tiled) {
+        // one group of waves where there are tiles for all anyway (577 x 4096 x 1024: 16.9 us, 20.5 with two), else two
+        // (256 x 4096 x 4096: 23.1 us, 24.2 with one; 577 x 1024 x 4096: 17.9, 23.0)
+        if (tiles_of(g, 64) > 512) launch_parts<TA, TB, EXACT, 1>(g, st);
+        else launch_parts<TA, TB, EXACT, 2>(g, st);
+    } else {
+        // Microseconds by what was measured: a stage of a round of tiles and what a round costs besides (8192 x 8192 x 8192 takes
+        // 517 us in 256 x 256 tiles and 628 in 128 x 128; 4096 x 4608 x 1152 51 and 40; 18464 x 4096 x 1024 109 and 110).
+        const double big = (double)((tiles_of(g, 256) + 255) / 256) * (2.0 * g.KB + 5.6),
+                     small = (double)((tiles_of(g, 128) + 511) / 512) * (1.225 * g.KB + 1.2);
+        if (EXACT || small < big) {
+            if (g.shiftB) launch_tile<TA, TB, EXACT, true, 128, 128, 64, 64>(g, 2, st);
+            else launch_tile<TA, TB, EXACT, false, 128, 128, 64, 64>(g, 2, st);
+        } else {
+            if (g.shiftB) launch_tile<TA, TB, false, true, 256, 256, 128, 64>(g, 1, st);
+            else launch_tile<TA, TB, false, false, 256, 256, 128, 64>(g, 1, st);
+        }
+    }
+    return hipGetLastError();
+}
 template <bool EXACT>
 static hipError_t launch_gemm_types(const GemmArgs &g, int typeA, int typeB, hipStream_t st) {
     if (typeA == SC_E4M3) return typeB == SC_E4M3 ? launch_gemm<0, 0, EXACT>(g, st) : launch_gemm<0, 1, EXACT>(g, st);
     return typeB == SC_E4M3 ? launch_gemm<1, 0, EXACT>(g, st) : launch_gemm<1, 1, EXACT>(g, st);
+}
+
+static GemmArgs gemm_args(const sc_fp8_gemm_desc &d) {
+    GemmArgs g{};
+    g.M = d.M;
+    g.N = d.N;
+    g.K = d.K;
+    g.KB = (d.K + FP8_BLOCK - 1) / FP8_BLOCK;
+    g.lda = d.lda;
+    g.ldb = d.ldb;
+    g.ldo = d.ldo;
+    g.strideA = d.strideA;
+    g.strideB = d.strideB;
+    g.strideO = d.strideO;
+    g.ldsA = d.ldsA;
+    g.ldsB = d.ldsB;
+    g.strideSA = d.strideSA;
+    g.strideSB = d.strideSB;
+    g.strideBias = d.strideBias;
+    g.shiftA = d.rowsA == 128 ? 7 : 0;
+    g.shiftB = d.rowsB == 128 ? 7 : 0;
+    g.typeO = d.typeO;
+    g.batch = d.batch;
+    return g;
 }
 
 static int check_gemm(const sc_fp8_gemm_desc *d) {
@@ -675,7 +906,7 @@ static int check_gemm(const sc_fp8_gemm_desc *d) {
         return SC_ERR_STRIDE;
     // (batch entries of the output must not lie on top of each other)
     if (d->batch > 1 && d->M > 0 && d->N > 0 && d->strideO < (int64_t)(d->M - 1) * d->ldo + d->N) return SC_ERR_STRIDE;
-    const int64_t tiles = (((int64_t)d->M + 63) / 64) * (((int64_t)d->N + 63) / 64);
+    const int64_t tiles = (((int64_t)d->M + 63) / 64) * (((int64_t)d->N + 31) / 32);
     if (tiles > INT32_MAX) return SC_ERR_SHAPE;
     return SC_OK;
 }
@@ -720,6 +951,10 @@ int sc_fp8_gemm_workspace_size(const sc_fp8_gemm_desc *desc, size_t *bytes) {
     const int rc = check_gemm(desc);
     if (rc != SC_OK) return rc;
     *bytes = 0;
+    if (desc->batch == 0 || desc->M == 0 || desc->N == 0) return SC_OK;
+    size_t a, b;
+    lay_sizes(gemm_args(*desc), &a, &b);
+    *bytes = a + b;
     return SC_OK;
 }
 
@@ -733,35 +968,22 @@ int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, co
     if (out == nullptr || (d.K > 0 && (A == nullptr || sA == nullptr || B == nullptr || sB == nullptr))) return SC_ERR_NULL;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned_to(workspace, 256))) return SC_ERR_WORKSPACE;
     if (!aligned_to(out, type_bytes(d.typeO)) || !aligned_to(sA, 4) || !aligned_to(sB, 4) || !aligned_to(bias, 4)) return SC_ERR_STRIDE;
-    GemmArgs g{};
-    g.M = d.M;
-    g.N = d.N;
-    g.K = d.K;
-    g.KB = (d.K + FP8_BLOCK - 1) / FP8_BLOCK;
+    GemmArgs g = gemm_args(d);
     g.A = static_cast<const uint8_t *>(A);
     g.B = static_cast<const uint8_t *>(B);
     g.sA = sA;
     g.sB = sB;
     g.bias = bias;
     g.out = out;
-    g.lda = d.lda;
-    g.ldb = d.ldb;
-    g.ldo = d.ldo;
-    g.strideA = d.strideA;
-    g.strideB = d.strideB;
-    g.strideO = d.strideO;
-    g.ldsA = d.ldsA;
-    g.ldsB = d.ldsB;
-    g.strideSA = d.strideSA;
-    g.strideSB = d.strideSB;
-    g.strideBias = d.strideBias;
-    g.shiftA = d.rowsA == 128 ? 7 : 0;
-    g.shiftB = d.rowsB == 128 ? 7 : 0;
-    g.typeO = d.typeO;
-    const int vb = 4 * type_bytes(d.typeO);
-    g.vecO = aligned_to(out, vb) && d.N % 4 == 0 && d.ldo % 4 == 0 && d.strideO % 4 == 0;
-    g.batch = d.batch;
+    const int eb = type_bytes(d.typeO), run = 16 / eb;       // outputs of a 16-byte store
+    g.whole = aligned_to(out, 16) && d.N % run == 0 && d.ldo % run == 0 && (d.batch == 1 || d.strideO % run == 0) && d.ldo <= 1 << 20;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    size_t la, lb;
+    lay_sizes(g, &la, &lb);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    if (la > 0 && lay(&g.A, &g.lda, &g.strideA, g.M, g, ws, st) != hipSuccess) return SC_ERR_HIP;
+    if (lb > 0 && lay(&g.B, &g.ldb, &g.strideB, g.N, g, ws + la, st) != hipSuccess) return SC_ERR_HIP;
+    if (la > 0 && lb > 0) g.K = g.KB * 128;         // (both operands have zeros there now)
     const hipError_t e = d.typeO == SC_F32 ? launch_gemm_types<true>(g, d.typeA, d.typeB, st) : launch_gemm_types<false>(g, d.typeA, d.typeB, st);
     return e == hipSuccess ? SC_OK : SC_ERR_HIP;
 }

@@ -12,7 +12,8 @@ namespace scl {
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef u4 u4_any __attribute__((aligned(1)));        // a 16-byte load from any address
+typedef u4 u4_any __attribute__((aligned(1)));        // 16 bytes at any address
+typedef u2 u2_any __attribute__((aligned(1)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float E4M3_MAX = 448.0f, E5M2_MAX = 57344.0f;

@@ -192,7 +192,8 @@ def test_fp8_gemm_views(scg):
     # operands, scales and result inside larger buffers, from odd bytes on; the rest stays as it was
     _note("fp8_gemm of views")
     gen = _gen(6)
-    for off, pad, M, N, K in ((0, 0, 150, 140, 256), (1, 3, 150, 140, 200), (16, 16, 270, 300, 384), (5, 11, 3, 333, 130), (16, 0, 40, 64, 256)):
+    for off, pad, M, N, K in ((0, 0, 150, 140, 256), (1, 3, 150, 140, 200), (16, 16, 270, 300, 384), (5, 11, 3, 333, 130), (16, 0, 40, 64, 256),
+                               (5, 11, 1500, 1411, 200), (1, 15, 1500, 1411, 240), (16, 16, 1500, 1411, 224)):
         A0, B0 = (torch.randint(0, 120, (n, K + off + pad), generator=gen, device="cuda", dtype=torch.uint8) for n in (M, N))
         kb = -(-K // 128)
         sA0, sB0 = torch.rand((M, kb + 2), generator=gen, device="cuda"), torch.rand((-(-N // 128), kb + 1), generator=gen, device="cuda")
