@@ -390,11 +390,12 @@ __device__ __forceinline__ void store_rows(uint8_t *corner, const float *bias, i
 #pragma unroll
             for (int h = 0; h < STEP; ++h) {
                 const f4 v = acc[i][j + h] + add[h];
+                if (TO == SC_F32) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (TO == SC_F32) w[e] = __float_as_uint(v[e]);
-                    else if (e & 1) w[2 * h + (e >> 1)] |= (TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e])) << 16;
-                    else w[2 * h + (e >> 1)] = TO == SC_BF16 ? to_bf16(v[e]) : to_f16(v[e]);
+                    for (int e = 0; e < 4; ++e) w[TO == SC_F32 ? e : 0] = __float_as_uint(v[e]);
+                } else {
+                    w[2 * h] = to_pair(TO, v[0], v[1]);
+                    w[2 * h + 1] = to_pair(TO, v[2], v[3]);
                 }
             }
             constexpr int WORDS = TO == SC_F32 ? 4 : 2 * STEP;

@@ -14,6 +14,7 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef u4 u4_any __attribute__((aligned(1)));        // 16 bytes at any address
 typedef u2 u2_any __attribute__((aligned(1)));
+typedef u4 u4_8 __attribute__((aligned(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr float E4M3_MAX = 448.0f, E5M2_MAX = 57344.0f;
@@ -24,9 +25,14 @@ inline bool is_fp8_type(int t) { return t == SC_E4M3 || t == SC_E5M2; }
 __host__ __device__ __forceinline__ int type_bytes(int t) { return t == SC_F32 ? 4 : t == SC_BF16 || t == SC_F16 ? 2 : 1; }
 inline bool aligned_to(const void *p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 
-// a float to the nearest bf16 or fp16, ties to even (one instruction each)
-__device__ __forceinline__ uint32_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-__device__ __forceinline__ uint32_t to_f16(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
+// Two floats to the nearest bf16 or fp16 values, ties to even, the first in the lower half
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 hf2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t to_pair(int type, float lo, float hi) {
+    if (type == SC_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), bf2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), hf2));
+}
 __device__ __forceinline__ float from_bf16(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float from_f16(uint32_t x) { return (float)__builtin_bit_cast(_Float16, (uint16_t)x); }
 
@@ -82,14 +88,13 @@ __device__ __forceinline__ void store4(int type, void *p, int64_t at, f4 v, int 
                 if (j < n) q[j] = v[j];
         }
     } else {
-        uint32_t h[4];
-        for (int j = 0; j < 4; ++j) h[j] = type == SC_BF16 ? to_bf16(v[j]) : to_f16(v[j]);
+        const u2 w = {to_pair(type, v[0], v[1]), to_pair(type, v[2], v[3])};
         uint16_t *q = static_cast<uint16_t *>(p) + at;
         if (VEC) {
-            *reinterpret_cast<u2 *>(q) = u2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+            *reinterpret_cast<u2 *>(q) = w;
         } else {
             for (int j = 0; j < 4; ++j)
-                if (j < n) q[j] = (uint16_t)h[j];
+                if (j < n) q[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
         }
     }
 }

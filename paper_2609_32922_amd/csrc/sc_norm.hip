@@ -21,17 +21,17 @@ struct NormArgs {
     int chunks;
 };
 
-// A block's threads: RPB rows side by side, W waves each
-template <int W>
+// A block's threads: RPB rows side by side, W waves each; MOST waves where rows are shorter
+template <int W, int MOST>
 struct Waves {
-    static constexpr int RPB = W >= 8 ? 1 : 8 / W, THREADS = W >= 8 ? 64 * W : 512;
+    static constexpr int RPB = W >= MOST ? 1 : MOST / W, THREADS = 64 * W * RPB;
 };
 
 // Sums of N values over a row; every thread of the row gets them.  Rows of several waves meet in LDS, in one of two places
 // by turns, so that one barrier is enough.
-template <int W, int N>
+template <int W, int N, int RPB>
 struct RowSums {
-    static constexpr int SLOT = N * Waves<W>::RPB * W;
+    static constexpr int SLOT = N * RPB * W;
     float *lds;
     int turn = 0;
     __device__ __forceinline__ void operator()(float (&v)[N], int n) {
@@ -117,20 +117,25 @@ struct RawRow {
         }
     }
 };
-// a parameter's row plus `off`, or `none` where there is no parameter
+// A parameter's row as it lies in memory, loaded ahead of its use
 template <int W, int NV, int R, bool VEC>
-__device__ __forceinline__ void load_param(f4 (&v)[NV], int type, const void *p, int64_t at, int t, int D, float off, float none) {
-    if (p == nullptr) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) v[k] = f4{none, none, none, none};
-        return;
-    }
+struct Param {
     RawRow<W, NV, R, VEC> r;
-    r.load(type, p, at, t, D);
-    r.widen(type, v);
+    __device__ __forceinline__ void load(int type, const void *p, int64_t at, int t, int D) {
+        if (p) r.load(type, p, at, t, D);
+    }
+    // plus `off`, or `none` where there is no parameter
+    __device__ __forceinline__ void get(f4 (&v)[NV], int type, const void *p, float off, float none) const {
+        if (p == nullptr) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] += off;
-}
+            for (int k = 0; k < NV; ++k) v[k] = f4{none, none, none, none};
+            return;
+        }
+        r.widen(type, v);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] += off;
+    }
+};
 template <int W, int NV, bool VEC>
 __device__ __forceinline__ void store_row(int type, void *p, int64_t at, int t, int D, const f4 (&v)[NV]) {
     if (type == SC_F32) {
@@ -168,21 +173,20 @@ __device__ __forceinline__ void centre(f4 (&v)[NV], float m, int t, int D) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[k][j] = 4 * (64 * W * k + t) + j < D ? v[k][j] - m : 0.0f;
 }
-// 1 / sqrt(mean + eps), to a rounding of each step
-__device__ __forceinline__ float inverse_deviation(float squares, float n, float eps) { return 1.0f / sqrtf(squares / n + eps); }
+__device__ __forceinline__ float inverse_deviation(float squares, float n_inv, float eps) { return rsqrtf(fmaf(squares, n_inv, eps)); }
 
 // v normalised in place (elements past D become 0).  The mean is taken before the squares, which therefore lose
 // nothing to it.
 template <int W, int NV, typename Sums>
-__device__ __forceinline__ void normalise(f4 (&v)[NV], int kind, float eps, int t, int D, Sums &sums) {
+__device__ __forceinline__ void normalise(f4 (&v)[NV], int kind, float eps, float n_inv, int t, int D, Sums &sums) {
     if (kind == SC_NORM_LAYER) {
         float s[1] = {sum(v)};
         sums(s, 1);
-        centre<W>(v, s[0] / (float)D, t, D);
+        centre<W>(v, s[0] * n_inv, t, D);
     }
     float q[1] = {dot(v, v)};
     sums(q, 1);
-    const float r = inverse_deviation(q[0], (float)D, eps);
+    const float r = inverse_deviation(q[0], n_inv, eps);
 #pragma unroll
     for (int k = 0; k < NV; ++k) v[k] *= r;
 }
@@ -190,11 +194,12 @@ __device__ __forceinline__ void normalise(f4 (&v)[NV], int kind, float eps, int 
 // One row by W waves, held in registers from its loads to its stores: every operand is read once and every
 // result written once.  Memory-bound.
 template <int W, int NV, int RX, int RY, bool VEC>
-__global__ __launch_bounds__(Waves<W>::THREADS) void k_norm(NormArgs a) {
-    constexpr int RPB = Waves<W>::RPB;
+__global__ __launch_bounds__((Waves<W, 4>::THREADS)) void k_norm(NormArgs a) {
+    constexpr int RPB = Waves<W, 4>::RPB;
     __shared__ float lds[2 * RPB * W];
-    RowSums<W, 1> sums{lds};
+    RowSums<W, 1, RPB> sums{lds};
     const int t = threadIdx.x % (64 * W), D = a.D;
+    const float n_inv = 1.0f / (float)D;
     const int64_t row = (int64_t)block_id() * RPB + threadIdx.x / (64 * W);
     const bool live = row < a.rows;
     if (W == 1 && !live) return;          // (rows of several waves meet at barriers, so all of a block's stay)
@@ -204,6 +209,10 @@ __global__ __launch_bounds__(Waves<W>::THREADS) void k_norm(NormArgs a) {
         RawRow<W, NV, RY, VEC> ry;
         rx.load(a.typeX, a.x, (int64_t)b * a.strideX + i * a.ldx, t, D);
         if (a.y) ry.load(a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
+        Param<W, NV, RY, VEC> gate, pre_w, pre_b;
+        if (a.y) gate.load(a.typeP, a.gate, (int64_t)b * a.s_gate, t, D);
+        pre_w.load(a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D);
+        pre_b.load(a.typeP, a.pre_b, (int64_t)b * a.s_pre_b, t, D);
         f4 x[NV];
         rx.widen(a.typeX, x);
 #pragma unroll
@@ -212,24 +221,27 @@ __global__ __launch_bounds__(Waves<W>::THREADS) void k_norm(NormArgs a) {
             f4 u[NV], w[NV];
             ry.widen(a.typeY, u);
             if (a.post != SC_NORM_NONE) {
-                normalise<W>(u, a.post, a.eps_post, t, D, sums);
+                Param<W, NV, RY, VEC> post_w, post_b;
+                post_w.load(a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D);
+                post_b.load(a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D);
+                normalise<W>(u, a.post, a.eps_post, n_inv, t, D, sums);
                 f4 c[NV];
-                load_param<W, NV, RY, VEC>(w, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
-                load_param<W, NV, RY, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
+                post_w.get(w, a.typeP, a.post_w, a.off_post, 1.0f);
+                post_b.get(c, a.typeP, a.post_b, 0.0f, 0.0f);
 #pragma unroll
                 for (int k = 0; k < NV; ++k) u[k] = u[k] * w[k] + c[k];
             }
-            load_param<W, NV, RY, VEC>(w, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
+            gate.get(w, a.typeP, a.gate, 0.0f, 1.0f);
 #pragma unroll
             for (int k = 0; k < NV; ++k) x[k] += u[k] * w[k];
         }
         if (a.xo && live) store_row<W, NV, VEC>(a.typeX, a.xo, (int64_t)b * a.strideXO + i * a.ldxo, t, D, x);
         if (a.h == nullptr) continue;
         if (a.pre != SC_NORM_NONE) {
-            normalise<W>(x, a.pre, a.eps_pre, t, D, sums);
+            normalise<W>(x, a.pre, a.eps_pre, n_inv, t, D, sums);
             f4 w[NV], c[NV];
-            load_param<W, NV, RY, VEC>(w, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
-            load_param<W, NV, RY, VEC>(c, a.typeP, a.pre_b, (int64_t)b * a.s_pre_b, t, D, 0.0f, 0.0f);
+            pre_w.get(w, a.typeP, a.pre_w, a.off_pre, 1.0f);
+            pre_b.get(c, a.typeP, a.pre_b, 0.0f, 0.0f);
 #pragma unroll
             for (int k = 0; k < NV; ++k) x[k] = x[k] * w[k] + c[k];
         }
@@ -290,11 +302,11 @@ enum { P_PRE_W, P_PRE_B, P_GATE, P_POST_W, P_POST_B, NPART };
 // gradient before it is r (d - n mean(d n)), LayerNorm also - mean(d); both means and the deviation come from one round of
 // sums.  POST: a norm behind the branch.  Memory-bound.
 template <int W, int NV, int RX, int RY, bool VEC, bool POST>
-__global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back(NormArgs a) {
-    constexpr int RPB = Waves<W>::RPB, NP = POST ? 5 : 3, NS = 4;
+__global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm_back(NormArgs a) {
+    constexpr int RPB = Waves<W, 8>::RPB, NP = POST ? 5 : 3, NS = 4;
     __shared__ float lds[2 * NS * RPB * W];
     __shared__ f4 join[RPB > 1 ? (RPB - 1) * 64 * W : 1];
-    RowSums<W, NS> sums{lds};
+    RowSums<W, NS, RPB> sums{lds};
     const int t = threadIdx.x % (64 * W), side = threadIdx.x / (64 * W), D = a.D;
     const int64_t chunk = block_id();
     if (chunk >= a.chunks) return;
@@ -316,6 +328,14 @@ __global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back
             if (a.dxo) rg.load(a.typeX, a.dxo, (int64_t)b * a.strideDXO + i * a.lddxo, t, D);
         };
         fetch(i0 + side);
+        // (the parameters are the same for all of the rows)
+        Param<W, NV, RY, VEC> pre_w, gate, post_w, post_b;
+        pre_w.load(a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D);
+        if (a.y || a.dy) gate.load(a.typeP, a.gate, (int64_t)b * a.s_gate, t, D);
+        if (POST) {
+            post_w.load(a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D);
+            post_b.load(a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D);
+        }
         for (int64_t first = i0; first < i1; first += RPB) {
             const int64_t i = first + side;
             const bool live = i < i1;               // (a row behind the last takes part in barriers and counts nothing)
@@ -345,7 +365,7 @@ __global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back
                 f4 d[NV];
                 float s[NS] = {0.0f, 0.0f, 0.0f, POST ? dot(m, m) : 0.0f};
                 if (pre) {
-                    load_param<W, NV, RY, VEC>(d, a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D, a.off_pre, 1.0f);
+                    pre_w.get(d, a.typeP, a.pre_w, a.off_pre, 1.0f);
 #pragma unroll
                     for (int k = 0; k < NV; ++k) d[k] *= g[k];
                     s[0] = dot(n, n);
@@ -353,9 +373,9 @@ __global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back
                     s[2] = sum(d);
                 }
                 sums(s, NS);
-                if (POST) r_post = inverse_deviation(s[3], (float)D, a.eps_post);
+                if (POST) r_post = inverse_deviation(s[3], n_inv, a.eps_post);
                 if (pre) {
-                    const float r = inverse_deviation(s[0], (float)D, a.eps_pre), dn = s[1] * r * n_inv,
+                    const float r = inverse_deviation(s[0], n_inv, a.eps_pre), dn = s[1] * r * n_inv,
                                 dm = pre_mean ? s[2] * n_inv : 0.0f;
 #pragma unroll
                     for (int k = 0; k < NV; ++k)
@@ -377,11 +397,11 @@ __global__ __launch_bounds__(Waves<W>::THREADS, W <= 8 ? 2 : 4) void k_norm_back
                 store_row<W, NV, VEC>(a.typeX, a.dx, (int64_t)b * a.strideX + i * a.ldx, t, D, e);
             }
             if (a.y == nullptr && a.dy == nullptr) continue;
-            load_param<W, NV, RY, VEC>(e, a.typeP, a.gate, (int64_t)b * a.s_gate, t, D, 0.0f, 1.0f);
+            gate.get(e, a.typeP, a.gate, 0.0f, 1.0f);
             if (POST) {
                 f4 pw[NV], c[NV];
-                load_param<W, NV, RY, VEC>(pw, a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D, a.off_post, 1.0f);
-                load_param<W, NV, RY, VEC>(c, a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D, 0.0f, 0.0f);
+                post_w.get(pw, a.typeP, a.post_w, a.off_post, 1.0f);
+                post_b.get(c, a.typeP, a.post_b, 0.0f, 0.0f);
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -468,12 +488,12 @@ enum { ANY_ANY, ANY_16, ALL_16 };     // types of the residual stream, and of th
 
 template <int W, int NV, int RX, int RY, bool VEC>
 static void launch_forward(const NormArgs &a, hipStream_t st) {
-    const uint32_t blocks = (uint32_t)(((int64_t)a.rows + Waves<W>::RPB - 1) / Waves<W>::RPB);
-    hipLaunchKernelGGL((k_norm<W, NV, RX, RY, VEC>), grid_of(blocks, a.batch), dim3(Waves<W>::THREADS), 0, st, a);
+    const uint32_t blocks = (uint32_t)(((int64_t)a.rows + Waves<W, 4>::RPB - 1) / Waves<W, 4>::RPB);
+    hipLaunchKernelGGL((k_norm<W, NV, RX, RY, VEC>), grid_of(blocks, a.batch), dim3(Waves<W, 4>::THREADS), 0, st, a);
 }
 template <int W, int NV, int RX, int RY, bool VEC>
 static void launch_backward(const NormArgs &a, hipStream_t st) {
-    const dim3 grid = grid_of((uint32_t)a.chunks, a.batch), block(Waves<W>::THREADS);
+    const dim3 grid = grid_of((uint32_t)a.chunks, a.batch), block(Waves<W, 8>::THREADS);
     if (a.post != SC_NORM_NONE) hipLaunchKernelGGL((k_norm_back<W, NV, RX, RY, VEC, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_norm_back<W, NV, RX, RY, VEC, false>), grid, block, 0, st, a);
 }
@@ -500,7 +520,8 @@ static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_
         else if (D <= 4096) launch_backward<8, 2, 4, 4, false>(a, st);
         else launch_backward<16, 4, 4, 4, false>(a, st);
     } else if (!vec) {
-        if (D <= 1280) launch_forward<1, 5, 4, 4, false>(a, st);
+        if (D <= 768) launch_forward<1, 3, 4, 4, false>(a, st);
+        else if (D <= 2048) launch_forward<4, 2, 4, 4, false>(a, st);
         else launch_forward<16, 4, 4, 4, false>(a, st);
     } else if (back) {
         if (D <= 512) backward_of<1, 2>(a, types, st);
@@ -512,11 +533,12 @@ static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_
         else backward_of<16, 4>(a, types, st);
     } else {
         if (D <= 512) forward_of<1, 2>(a, types, st);
-        else if (D <= 1024) forward_of<1, 4>(a, types, st);
-        else if (D <= 1280) forward_of<1, 5>(a, types, st);
-        else if (D <= 2048) forward_of<2, 4>(a, types, st);
-        else if (D <= 4096) forward_of<4, 4>(a, types, st);
-        else if (D <= 8192) forward_of<8, 4>(a, types, st);
+        else if (D <= 768) forward_of<1, 3>(a, types, st);
+        else if (D <= 1024) forward_of<2, 2>(a, types, st);
+        else if (D <= 1536) forward_of<2, 3>(a, types, st);
+        else if (D <= 2048) forward_of<4, 2>(a, types, st);
+        else if (D <= 4096) forward_of<8, 2>(a, types, st);
+        else if (D <= 8192) forward_of<16, 2>(a, types, st);
         else forward_of<16, 4>(a, types, st);
     }
     return hipGetLastError();

@@ -15,8 +15,7 @@ struct RopeArgs {
     float *scale, *rowmax;
     int groups;              // threads of a head's row: each has four pairs, or eight elements that pass
     int turning;             // of these, those with pairs
-    int heads_each;          // heads that a thread takes one after the other
-    int hblocks;             // groups of heads
+    int each, hblocks;       // heads of a thread, and groups of them
 };
 
 // cosine and sine of four pairs of a token.  The turn n = pos freq / 2 pi is formed as an unevaluated sum of two float64
@@ -43,16 +42,44 @@ __device__ __forceinline__ void turns(const RopeArgs &a, int b, int64_t token, i
     }
 }
 
-// A thread has four pairs of a token (or eight elements that pass) and takes them through heads_each heads with one
-// set of cosines.  Memory-bound.  VEC: rows, pairs and halves on four elements.
-template <bool VEC, bool NEAR>
-__global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int G) {
+// A head's eight elements of a thread, two quads, as they lie in memory.  R: words of a quad, 2 where the type has 16 bits, 4
+// where it is float32.
+template <int R, bool VEC, bool NEAR>
+struct Eight {
+    uint32_t w[2 * R];
+    __device__ __forceinline__ void load(const void *p, int64_t at, int e0, int e1, int n0, int n1) {
+        if (VEC && NEAR && R == 2 && n1 > 0) {      // the quads are neighbours: one 16-byte load
+            const u4 x = *reinterpret_cast<const u4_8 *>(static_cast<const uint16_t *>(p) + at + e0);
+#pragma unroll
+            for (int j = 0; j < 2 * R; ++j) w[j] = x[j & 3];
+            return;
+        }
+        const Raw4 a = load_raw<VEC>(R == 4 ? SC_F32 : SC_BF16, p, at + e0, n0), b = load_raw<VEC>(R == 4 ? SC_F32 : SC_BF16, p, at + e1, n1);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            w[j] = a.w[j];
+            w[R + j] = b.w[j];
+        }
+    }
+    __device__ __forceinline__ f4 quad(int type, int h) const {
+        Raw4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r.w[j] = w[h * R + (j < R ? j : 0)];
+        return to_floats(R == 4 ? SC_F32 : type, r);
+    }
+};
+
+// A thread has four pairs of a token (or eight elements that pass) and takes them through a.each heads with one set of cosines,
+// HEADS of them at a time, the next ones' loads in flight.  Memory-bound.  VEC: rows, pairs and halves on four elements.
+constexpr int HEADS = 4;
+template <bool VEC, bool NEAR, int R>
+__global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int shift) {
     const sc_rope_desc &d = a.d;
     if (block_id() >= blocks) return;
-    const int sub = threadIdx.x % G;
-    const int64_t unit = (int64_t)block_id() * (256 / G) + threadIdx.x / G;
+    const int G = 1 << shift, sub = threadIdx.x & (G - 1);
+    const int64_t unit = ((int64_t)block_id() << (8 - shift)) + (threadIdx.x >> shift);
     const int64_t token = unit / a.hblocks;
-    const int h0 = (int)(unit % a.hblocks) * a.heads_each, h1 = min(h0 + a.heads_each, d.heads);
+    const int h0 = (int)(unit - token * a.hblocks) * a.each, h1 = min(h0 + a.each, d.heads);
     const bool live = token < d.tokens && sub < a.groups;
     const int P = d.pairs, p0 = 4 * sub, tail = 2 * P + 8 * (sub - a.turning);
     // the two quads of a thread: where they start and how many elements they have
@@ -61,12 +88,24 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int G
     const int n0 = !live ? 0 : !turn ? min(d.D - e0, 4) : NEAR ? min(2 * P - e0, 4) : min(P - p0, 4);
     const int n1 = !live ? 0 : !turn ? min(d.D - e1, 4) : NEAR ? min(2 * P - e1, 4) : min(P - p0, 4);
     for (int b = blockIdx.z; b < d.batch; b += gridDim.z) {
+        const int64_t from = (int64_t)b * d.strideXB + token * d.strideXT, to = (int64_t)b * d.strideOB + token * d.strideOT;
+        Eight<R, VEC, NEAR> next[HEADS];
+        const auto load = [&](int first) {
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h)
+                next[h].load(a.x, from + (int64_t)(first + h) * d.strideXH, e0, e1, first + h < h1 ? n0 : 0, first + h < h1 ? n1 : 0);
+        };
+        load(h0);
         f4 c = {1.0f, 1.0f, 1.0f, 1.0f}, s = {0.0f, 0.0f, 0.0f, 0.0f};
         if (live && turn) turns(a, b, token, p0, c, s);
-        for (int h = h0; h < h1; ++h) {
-            const int64_t at = (int64_t)b * d.strideXB + token * d.strideXT + (int64_t)h * d.strideXH;
-            f4 u = to_floats(d.typeX, load_raw<VEC>(d.typeX, a.x, at + e0, n0));
-            f4 v = to_floats(d.typeX, load_raw<VEC>(d.typeX, a.x, at + e1, n1));
+        for (int first = h0; first < h1; first += HEADS) {
+            Eight<R, VEC, NEAR> x[HEADS];
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) x[h] = next[h];
+            load(first + HEADS);
+#pragma unroll
+          for (int h = 0; h < HEADS; ++h) {
+            const f4 u = x[h].quad(d.typeX, 0), v = x[h].quad(d.typeX, 1);
             f4 o0 = u, o1 = v;
             if (turn) {
                 if (NEAR) {
@@ -80,27 +119,41 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int G
                     }
                 }
             }
-            const int64_t to = (int64_t)b * d.strideOB + token * d.strideOT + (int64_t)h * d.strideOH;
+            const int64_t at = to + (int64_t)(first + h) * d.strideOH;
+            const int k0 = first + h < h1 ? n0 : 0, k1 = first + h < h1 ? n1 : 0;
             if (d.typeO == SC_INT8) {
                 float m = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (j < n0) m = fmaxf(m, fabsf(o0[j]));
-                    if (j < n1) m = fmaxf(m, fabsf(o1[j]));
+                    if (j < k0) m = fmaxf(m, fabsf(o0[j]));
+                    if (j < k1) m = fmaxf(m, fabsf(o1[j]));
                 }
                 for (int o = G / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
                 const float sc = m / 127.0f;
-                if (live && sub == 0) {
-                    const int64_t si = (int64_t)b * d.strideSB + token * d.strideST + (int64_t)h * d.strideSH;
+                if (live && sub == 0 && first + h < h1) {
+                    const int64_t si = (int64_t)b * d.strideSB + token * d.strideST + (int64_t)(first + h) * d.strideSH;
                     a.scale[si] = sc;
                     if (a.rowmax) a.rowmax[si] = m;
                 }
-                store_bytes4<VEC>(a.out, to + e0, quant_int8x4(o0, sc), n0);
-                store_bytes4<VEC>(a.out, to + e1, quant_int8x4(o1, sc), n1);
+                store_bytes4<VEC>(a.out, at + e0, quant_int8x4(o0, sc), k0);
+                store_bytes4<VEC>(a.out, at + e1, quant_int8x4(o1, sc), k1);
+            } else if (VEC && NEAR && d.typeO != SC_F32) {
+                if (k1 > 0) {
+                    u4 w;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float lo = j < 2 ? o0[2 * (j & 1)] : o1[2 * (j & 1)], hi = j < 2 ? o0[2 * (j & 1) + 1] : o1[2 * (j & 1) + 1];
+                        w[j] = to_pair(d.typeO, lo, hi);
+                    }
+                    *reinterpret_cast<u4_8 *>(static_cast<uint16_t *>(a.out) + at + e0) = w;
+                } else {
+                    store4<VEC>(d.typeO, a.out, at + e0, o0, k0);
+                }
             } else {
-                store4<VEC>(d.typeO, a.out, to + e0, o0, n0);
-                store4<VEC>(d.typeO, a.out, to + e1, o1, n1);
+                store4<VEC>(d.typeO, a.out, at + e0, o0, k0);
+                store4<VEC>(d.typeO, a.out, at + e1, o1, k1);
             }
+          }
         }
     }
 }
@@ -125,6 +178,12 @@ static bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, in
         span += (n[i] - 1) * s[i];
     }
     return true;
+}
+
+template <bool VEC, int R>
+static void launch_rope(const RopeArgs &a, bool near, dim3 grid, uint32_t blocks, int shift, hipStream_t st) {
+    if (near) hipLaunchKernelGGL((k_rope<VEC, true, R>), grid, dim3(256), 0, st, a, blocks, shift);
+    else hipLaunchKernelGGL((k_rope<VEC, false, R>), grid, dim3(256), 0, st, a, blocks, shift);
 }
 
 }  // namespace scl
@@ -168,11 +227,12 @@ extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *p
     a.groups = a.turning + (d.D - 2 * d.pairs + 7) / 8;
     if (a.groups < 1) a.groups = 1;
     // (at most 33 groups, so a head's row lies in one wave, whose lanes take an int8 row's maximum)
-    int G = 1;
-    while (G < a.groups) G <<= 1;
-    a.heads_each = 4;
-    a.hblocks = (d.heads + a.heads_each - 1) / a.heads_each;
-    const int64_t units = (int64_t)d.tokens * a.hblocks, blocks = (units + 256 / G - 1) / (256 / G);
+    int shift = 0;
+    while (1 << shift < a.groups) ++shift;
+    // all heads by one thread, whose cosines are then computed once, where tokens are enough for every compute unit
+    a.each = ((int64_t)d.tokens << shift) * (d.batch < 32768 ? d.batch : 32768) >= 256 * 512 ? (d.heads + HEADS - 1) / HEADS * HEADS : HEADS;
+    a.hblocks = (int)(((int64_t)d.heads + a.each - 1) / a.each);
+    const int64_t units = (int64_t)d.tokens * a.hblocks, blocks = (units + (256 >> shift) - 1) / (256 >> shift);
     if (blocks > INT32_MAX) return SC_ERR_SHAPE;
     const int64_t xb = 4 * type_bytes(d.typeX), ob = 4 * type_bytes(d.typeO);
     const bool vec = d.D % 4 == 0 && d.pairs % 4 == 0 && aligned_to(x, xb) && aligned_to(out, ob) &&
@@ -180,13 +240,11 @@ extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *p
                      d.strideOT % 4 == 0 && d.strideOH % 4 == 0;
     const dim3 grid = grid_of((uint32_t)blocks, d.batch);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const bool near = d.pairing == SC_ROPE_NEIGHBOURS;
-    if (vec) {
-        if (near) hipLaunchKernelGGL((k_rope<true, true>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
-        else hipLaunchKernelGGL((k_rope<true, false>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
-    } else {
-        if (near) hipLaunchKernelGGL((k_rope<false, true>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
-        else hipLaunchKernelGGL((k_rope<false, false>), grid, dim3(256), 0, st, a, (uint32_t)blocks, G);
-    }
+    const bool near = d.pairing == SC_ROPE_NEIGHBOURS, wide = d.typeX == SC_F32;
+    const uint32_t n = (uint32_t)blocks;
+    if (vec && wide) launch_rope<true, 4>(a, near, grid, n, shift, st);
+    else if (vec) launch_rope<true, 2>(a, near, grid, n, shift, st);
+    else if (wide) launch_rope<false, 4>(a, near, grid, n, shift, st);
+    else launch_rope<false, 2>(a, near, grid, n, shift, st);
     return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP;
 }
