@@ -76,13 +76,15 @@ __device__ __forceinline__ f4 to_floats(int type, const Raw4 &r) {
     }
     return v;
 }
-template <bool VEC>
+// (STREAM: past the caches)
+template <bool VEC, bool STREAM = false>
 __device__ __forceinline__ void store4(int type, void *p, int64_t at, f4 v, int n) {
     if (n <= 0) return;
     if (type == SC_F32) {
         float *q = static_cast<float *>(p) + at;
         if (VEC) {
-            *reinterpret_cast<f4 *>(q) = v;
+            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<f4 *>(q));
+            else *reinterpret_cast<f4 *>(q) = v;
         } else {
             for (int j = 0; j < 4; ++j)
                 if (j < n) q[j] = v[j];
@@ -91,7 +93,8 @@ __device__ __forceinline__ void store4(int type, void *p, int64_t at, f4 v, int 
         const u2 w = {to_pair(type, v[0], v[1]), to_pair(type, v[2], v[3])};
         uint16_t *q = static_cast<uint16_t *>(p) + at;
         if (VEC) {
-            *reinterpret_cast<u2 *>(q) = w;
+            if (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<u2 *>(q));
+            else *reinterpret_cast<u2 *>(q) = w;
         } else {
             for (int j = 0; j < 4; ++j)
                 if (j < n) q[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));

@@ -58,11 +58,52 @@ struct RowSums {
     }
 };
 
-// A row's elements as they lie in memory, NV quads a thread: quad k of thread t is elements 4 (64 W k + t) .. + 3.  R: words of
+// A row of a tensor for buffer instructions, whose bound drops what lies behind the row: loads of it give 0 and stores of it
+// do nothing, so no lane branches.  The rows of a wave are the same in all of its lanes.  There is none where p is null.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer row_of(const void *p, int type, int b, int64_t stride, int64_t i, int64_t ld, int D, bool there = true) {
+    const int es = type_bytes(type);
+    return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t *>(const_cast<void *>(p)) + (b * stride + i * ld) * es, 0,
+                                             p != nullptr && there ? D * es : 0, 0x00020000);
+}
+// Its elements as they lie in memory, NV quads a thread: quad k of thread t is elements 4 (64 W k + t) .. + 3.  R: words of
 // a quad, 2 where the type has 16 bits, 4 where it may be any.
 template <int W, int NV, int R, bool VEC>
 struct RawRow {
     uint32_t w[NV][R];
+    __device__ __forceinline__ void load(int type, Buffer p, int t) {
+        if (R == 4 && type == SC_F32) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int at = 16 * (64 * W * k + t);
+                if (VEC) {
+                    const u4 x = __builtin_amdgcn_raw_buffer_load_b128(p, at, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < R; ++j) w[k][j] = x[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < R; ++j) w[k][j] = __builtin_amdgcn_raw_buffer_load_b32(p, at + 4 * j, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int at = 8 * (64 * W * k + t);
+                if (VEC) {
+                    const u2 x = __builtin_amdgcn_raw_buffer_load_b64(p, at, 0, 0);
+                    w[k][0] = x[0];
+                    w[k][1] = x[1];
+                } else {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(p, at + 2 * j, 0, 0);
+                    w[k][0] = h[0] | h[1] << 16;
+                    w[k][1] = h[2] | h[3] << 16;
+                }
+            }
+        }
+    }
+    // the same by address, with the lanes behind the row's end masked
     __device__ __forceinline__ void load(int type, const void *p, int64_t at, int t, int D) {
         if (R == 4 && type == SC_F32) {
             const uint32_t *q = static_cast<const uint32_t *>(p) + at;
@@ -124,6 +165,9 @@ struct Param {
     __device__ __forceinline__ void load(int type, const void *p, int64_t at, int t, int D) {
         if (p) r.load(type, p, at, t, D);
     }
+    __device__ __forceinline__ void load_row(int type, const void *p, int b, int64_t stride, int t, int D) {
+        if (p) r.load(type, row_of(p, type, b, stride, 0, 0, D), t);
+    }
     // plus `off`, or `none` where there is no parameter
     __device__ __forceinline__ void get(f4 (&v)[NV], int type, const void *p, float off, float none) const {
         if (p == nullptr) {
@@ -136,6 +180,40 @@ struct Param {
         for (int k = 0; k < NV; ++k) v[k] += off;
     }
 };
+template <int W, int NV, bool VEC>
+__device__ __forceinline__ void store_row(int type, Buffer p, int t, const f4 (&v)[NV]) {
+    if (type == SC_F32) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = 16 * (64 * W * k + t);
+            if (VEC) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v[k]), p, at, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[k][j]), p, at + 4 * j, 0, 0);
+            }
+        }
+    } else {
+        u2 w[NV];
+        if (type == SC_BF16) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) w[k] = u2{to_pair(SC_BF16, v[k][0], v[k][1]), to_pair(SC_BF16, v[k][2], v[k][3])};
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) w[k] = u2{to_pair(SC_F16, v[k][0], v[k][1]), to_pair(SC_F16, v[k][2], v[k][3])};
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = 8 * (64 * W * k + t);
+            if (VEC) {
+                __builtin_amdgcn_raw_buffer_store_b64(w[k], p, at, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[k][j >> 1] >> (16 * (j & 1))), p, at + 2 * j, 0, 0);
+            }
+        }
+    }
+}
 template <int W, int NV, bool VEC>
 __device__ __forceinline__ void store_row(int type, void *p, int64_t at, int t, int D, const f4 (&v)[NV]) {
     if (type == SC_F32) {
@@ -307,7 +385,7 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
     __shared__ float lds[2 * NS * RPB * W];
     __shared__ f4 join[RPB > 1 ? (RPB - 1) * 64 * W : 1];
     RowSums<W, NS, RPB> sums{lds};
-    const int t = threadIdx.x % (64 * W), side = threadIdx.x / (64 * W), D = a.D;
+    const int t = threadIdx.x % (64 * W), side = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)), D = a.D;
     const int64_t chunk = block_id();
     if (chunk >= a.chunks) return;
     const int64_t i0 = chunk * a.rows / a.chunks, i1 = (chunk + 1) * a.rows / a.chunks;
@@ -320,37 +398,32 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
             for (int k = 0; k < NV; ++k) acc[p][k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         RawRow<W, NV, RX, VEC> rx, rg;
         RawRow<W, NV, RY, VEC> ry, rh;
-        const auto fetch = [&](int64_t row) {
-            const int64_t i = min(row, i1 - 1);
-            if (a.x) rx.load(a.typeX, a.x, (int64_t)b * a.strideXO + i * a.ldxo, t, D);
-            if (a.dh) rh.load(a.typeH, a.dh, (int64_t)b * a.strideH + i * a.ldh, t, D);
-            if (a.y) ry.load(a.typeY, a.y, (int64_t)b * a.strideY + i * a.ldy, t, D);
-            if (a.dxo) rg.load(a.typeX, a.dxo, (int64_t)b * a.strideDXO + i * a.lddxo, t, D);
+        // (a row that is not there is one of zeros)
+        const auto fetch = [&](int64_t i) {
+            const bool live = i < i1;
+            rx.load(a.typeX, row_of(a.x, a.typeX, b, a.strideXO, i, a.ldxo, D, live), t);
+            rh.load(a.typeH, row_of(a.dh, a.typeH, b, a.strideH, i, a.ldh, D, live), t);
+            ry.load(a.typeY, row_of(a.y, a.typeY, b, a.strideY, i, a.ldy, D, live), t);
+            rg.load(a.typeX, row_of(a.dxo, a.typeX, b, a.strideDXO, i, a.lddxo, D, live), t);
         };
         fetch(i0 + side);
         // (the parameters are the same for all of the rows)
         Param<W, NV, RY, VEC> pre_w, gate, post_w, post_b;
-        pre_w.load(a.typeP, a.pre_w, (int64_t)b * a.s_pre_w, t, D);
-        if (a.y || a.dy) gate.load(a.typeP, a.gate, (int64_t)b * a.s_gate, t, D);
+        pre_w.load_row(a.typeP, a.pre_w, b, a.s_pre_w, t, D);
+        if (a.y || a.dy) gate.load_row(a.typeP, a.gate, b, a.s_gate, t, D);
         if (POST) {
-            post_w.load(a.typeP, a.post_w, (int64_t)b * a.s_post_w, t, D);
-            post_b.load(a.typeP, a.post_b, (int64_t)b * a.s_post_b, t, D);
+            post_w.load_row(a.typeP, a.post_w, b, a.s_post_w, t, D);
+            post_b.load_row(a.typeP, a.post_b, b, a.s_post_b, t, D);
         }
         for (int64_t first = i0; first < i1; first += RPB) {
             const int64_t i = first + side;
             const bool live = i < i1;               // (a row behind the last takes part in barriers and counts nothing)
             if (W == 1 && !live) break;
             f4 n[NV], g[NV], e[NV], m[NV];
-            if (a.x) rx.widen(a.typeX, n);
-            if (a.dh) rh.widen(a.typeH, g);
-            if (a.y) ry.widen(a.typeY, m);
-            if (a.dxo) rg.widen(a.typeX, e);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (!a.dh || !live) g[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (!a.dxo || !live) e[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (!a.y) m[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-            }
+            rx.widen(a.typeX, n);
+            rh.widen(a.typeH, g);
+            ry.widen(a.typeY, m);
+            rg.widen(a.typeX, e);
             fetch(i + RPB);
             const bool pre = a.pre != SC_NORM_NONE && a.dh, pre_mean = pre && a.pre == SC_NORM_LAYER,
                        post_mean = POST && a.post == SC_NORM_LAYER;
@@ -391,10 +464,10 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
             if (!pre)
 #pragma unroll
                 for (int k = 0; k < NV; ++k) g[k] += e[k];
-            if (a.dx && live) {
+            if (a.dx) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k) e[k] = a.scale_res * g[k];
-                store_row<W, NV, VEC>(a.typeX, a.dx, (int64_t)b * a.strideX + i * a.ldx, t, D, e);
+                store_row<W, NV, VEC>(a.typeX, row_of(a.dx, a.typeX, b, a.strideX, i, a.ldx, D, live), t, e);
             }
             if (a.y == nullptr && a.dy == nullptr) continue;
             gate.get(e, a.typeP, a.gate, 0.0f, 1.0f);
@@ -429,7 +502,7 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
                         g[k][j] *= e[k][j];
                     }
             }
-            if (a.dy && live) store_row<W, NV, VEC>(a.typeY, a.dy, (int64_t)b * a.strideDY + i * a.lddy, t, D, g);
+            if (a.dy) store_row<W, NV, VEC>(a.typeY, row_of(a.dy, a.typeY, b, a.strideDY, i, a.lddy, D, live), t, g);
         }
         if (a.part == nullptr) continue;
         float *part = a.part + ((int64_t)b * a.chunks + chunk) * NPART * D;
@@ -455,11 +528,12 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
     }
 }
 
-// Sums over the chunks, and over the batch where a parameter is shared: 64 columns by 16 groups of chunks, whose
+// Sums over the chunks, and over the batch where a parameter is shared: COLS columns by GROUPS groups of chunks, whose
 // sums are joined in order
-__global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a) {
-    __shared__ float join[16][64];
-    const int c = threadIdx.x & 63, grp = threadIdx.x >> 6, d = blockIdx.x * 64 + c, p = blockIdx.y;
+template <int COLS, int GROUPS>
+__global__ __launch_bounds__(COLS * GROUPS) void k_norm_sums(NormArgs a) {
+    __shared__ float join[GROUPS][COLS];
+    const int c = threadIdx.x % COLS, grp = threadIdx.x / COLS, d = blockIdx.x * COLS + c, p = blockIdx.y;
     float *out = p == P_PRE_W ? a.dpre_w : p == P_PRE_B ? a.dpre_b : p == P_GATE ? a.dgate : p == P_POST_W ? a.dpost_w : a.dpost_b;
     const int64_t stride = p == P_PRE_W ? a.s_pre_w : p == P_PRE_B ? a.s_pre_b : p == P_GATE ? a.s_gate : p == P_POST_W ? a.s_post_w : a.s_post_b;
     if (out == nullptr) return;
@@ -469,13 +543,13 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a) {
         float s = 0.0f;
         if (d < a.D)
 #pragma unroll 8
-            for (int64_t k = grp; k < n; k += 16) s += q[k * NPART * a.D];
+            for (int64_t k = grp; k < n; k += GROUPS) s += q[k * NPART * a.D];
         __syncthreads();
         join[grp][c] = s;
         __syncthreads();
         if (grp == 0 && d < a.D) {
             s = 0.0f;
-            for (int k = 0; k < 16; ++k) s += join[k][c];
+            for (int k = 0; k < GROUPS; ++k) s += join[k][c];
             out[b * a.D + d] = s;      // (b = 0 where shared)
         }
     }
@@ -517,11 +591,13 @@ static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_
     const int types = x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;
     if (!vec && back) {
         if (D <= 512) launch_backward<1, 2, 4, 4, false>(a, st);
+        else if (D <= 1536) launch_backward<2, 3, 4, 4, false>(a, st);
         else if (D <= 4096) launch_backward<8, 2, 4, 4, false>(a, st);
         else launch_backward<16, 4, 4, 4, false>(a, st);
     } else if (!vec) {
         if (D <= 768) launch_forward<1, 3, 4, 4, false>(a, st);
-        else if (D <= 2048) launch_forward<4, 2, 4, 4, false>(a, st);
+        else if (D <= 1536) launch_forward<2, 3, 4, 4, false>(a, st);
+        else if (D <= 4096) launch_forward<8, 2, 4, 4, false>(a, st);
         else launch_forward<16, 4, 4, 4, false>(a, st);
     } else if (back) {
         if (D <= 512) backward_of<1, 2>(a, types, st);
@@ -529,7 +605,7 @@ static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_
         else if (D <= 1536) backward_of<2, 3>(a, types, st);
         else if (D <= 2048) backward_of<4, 2>(a, types, st);
         else if (D <= 4096) backward_of<8, 2>(a, types, st);
-        else if (D <= 8192) backward_of<16, 2>(a, types, st);
+        else if (D <= 8192) backward_of<8, 4>(a, types, st);
         else backward_of<16, 4>(a, types, st);
     } else {
         if (D <= 512) forward_of<1, 2>(a, types, st);
@@ -736,8 +812,12 @@ int sc_residual_norm_backward(const sc_norm_desc *desc, const void *xo, const vo
     if (rows && launch_rows(a, true, vec, st) != hipSuccess) return SC_ERR_HIP;
     // (without rows the sums are zeros)
     if (any) {
-        hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((d.D + 63) / 64), NPART, (unsigned)(d.batch < 1 ? 1 : d.batch < 32768 ? d.batch : 32768)),
-                           dim3(1024), 0, st, a);
+        const unsigned entries = d.batch < 1 ? 1 : d.batch < 32768 ? d.batch : 32768;
+        // (few chunks and many entries: a thread a column; else 32 groups)
+        if (a.chunks <= 32 && d.batch >= 8 && a.s_gate && a.s_pre_w)
+            hipLaunchKernelGGL((k_norm_sums<64, 4>), dim3((unsigned)((d.D + 63) / 64), NPART, entries), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((k_norm_sums<32, 32>), dim3((unsigned)((d.D + 31) / 32), NPART, entries), dim3(1024), 0, st, a);
         if (hipGetLastError() != hipSuccess) return SC_ERR_HIP;
     }
     return SC_OK;

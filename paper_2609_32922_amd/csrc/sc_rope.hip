@@ -71,8 +71,9 @@ struct Eight {
 
 // A thread has four pairs of a token (or eight elements that pass) and takes them through a.each heads with one set of cosines,
 // HEADS of them at a time, the next ones' loads in flight.  Memory-bound.  VEC: rows, pairs and halves on four elements.
+// STREAM: stores that do not stay in the caches.
 constexpr int HEADS = 4;
-template <bool VEC, bool NEAR, int R>
+template <bool VEC, bool NEAR, int R, bool STREAM>
 __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int shift) {
     const sc_rope_desc &d = a.d;
     if (block_id() >= blocks) return;
@@ -145,13 +146,15 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int s
                         const float lo = j < 2 ? o0[2 * (j & 1)] : o1[2 * (j & 1)], hi = j < 2 ? o0[2 * (j & 1) + 1] : o1[2 * (j & 1) + 1];
                         w[j] = to_pair(d.typeO, lo, hi);
                     }
-                    *reinterpret_cast<u4_8 *>(static_cast<uint16_t *>(a.out) + at + e0) = w;
+                    u4_8 *q = reinterpret_cast<u4_8 *>(static_cast<uint16_t *>(a.out) + at + e0);
+                    if (STREAM) __builtin_nontemporal_store(w, q);
+                    else *q = w;
                 } else {
-                    store4<VEC>(d.typeO, a.out, at + e0, o0, k0);
+                    store4<VEC, STREAM>(d.typeO, a.out, at + e0, o0, k0);
                 }
             } else {
-                store4<VEC>(d.typeO, a.out, at + e0, o0, k0);
-                store4<VEC>(d.typeO, a.out, at + e1, o1, k1);
+                store4<VEC, STREAM>(d.typeO, a.out, at + e0, o0, k0);
+                store4<VEC, STREAM>(d.typeO, a.out, at + e1, o1, k1);
             }
           }
         }
@@ -180,10 +183,10 @@ static bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, in
     return true;
 }
 
-template <bool VEC, int R>
+template <bool VEC, int R, bool STREAM>
 static void launch_rope(const RopeArgs &a, bool near, dim3 grid, uint32_t blocks, int shift, hipStream_t st) {
-    if (near) hipLaunchKernelGGL((k_rope<VEC, true, R>), grid, dim3(256), 0, st, a, blocks, shift);
-    else hipLaunchKernelGGL((k_rope<VEC, false, R>), grid, dim3(256), 0, st, a, blocks, shift);
+    if (near) hipLaunchKernelGGL((k_rope<VEC, true, R, STREAM>), grid, dim3(256), 0, st, a, blocks, shift);
+    else hipLaunchKernelGGL((k_rope<VEC, false, R, STREAM>), grid, dim3(256), 0, st, a, blocks, shift);
 }
 
 }  // namespace scl
@@ -242,9 +245,20 @@ extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *p
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const bool near = d.pairing == SC_ROPE_NEIGHBOURS, wide = d.typeX == SC_F32;
     const uint32_t n = (uint32_t)blocks;
-    if (vec && wide) launch_rope<true, 4>(a, near, grid, n, shift, st);
-    else if (vec) launch_rope<true, 2>(a, near, grid, n, shift, st);
-    else if (wide) launch_rope<false, 4>(a, near, grid, n, shift, st);
-    else launch_rope<false, 2>(a, near, grid, n, shift, st);
+    // A result that the caches do not hold until it is read anyway (256 MB at most, half of them its source) is stored past them:
+    // 24960 x 24 x 128 in 16 bits 74 -> 62 us.  One that they hold is not: 8192 x 8 x 256 in 32 bits takes 26 us either way, and
+    // its reader finds it there.
+    const bool stream_past = (int64_t)d.batch * d.tokens * d.heads * d.D * type_bytes(d.typeO) > (int64_t)128 << 20;
+    if (vec && wide) {
+        if (stream_past) launch_rope<true, 4, true>(a, near, grid, n, shift, st);
+        else launch_rope<true, 4, false>(a, near, grid, n, shift, st);
+    } else if (vec) {
+        if (stream_past) launch_rope<true, 2, true>(a, near, grid, n, shift, st);
+        else launch_rope<true, 2, false>(a, near, grid, n, shift, st);
+    } else if (wide) {
+        launch_rope<false, 4, false>(a, near, grid, n, shift, st);
+    } else {
+        launch_rope<false, 2, false>(a, near, grid, n, shift, st);
+    }
     return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP;
 }
