@@ -383,7 +383,7 @@ template <int W, int NV, int RX, int RY, bool VEC, bool POST>
 __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm_back(NormArgs a) {
     constexpr int RPB = Waves<W, 8>::RPB, NP = POST ? 5 : 3, NS = 4;
     __shared__ float lds[2 * NS * RPB * W];
-    __shared__ f4 join[RPB > 1 ? (RPB - 1) * 64 * W : 1];
+    __shared__ f4 join[RPB > 1 ? RPB : 1][RPB > 1 ? NP * NV : 1][64 * W];
     RowSums<W, NS, RPB> sums{lds};
     const int t = threadIdx.x % (64 * W), side = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)), D = a.D;
     const int64_t chunk = block_id();
@@ -505,24 +505,31 @@ __global__ __launch_bounds__((Waves<W, 8>::THREADS), W <= 8 ? 2 : 4) void k_norm
             if (a.dy) store_row<W, NV, VEC>(a.typeY, row_of(a.dy, a.typeY, b, a.strideDY, i, a.lddy, D, live), t, g);
         }
         if (a.part == nullptr) continue;
+        // The rows side by side join their sums in LDS, each side the ones of every RPB-th quad
         float *part = a.part + ((int64_t)b * a.chunks + chunk) * NPART * D;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
+        const auto put = [&](int p, int k, f4 v) {
             const bool wanted = p == P_PRE_W ? a.dpre_w != nullptr : p == P_PRE_B ? a.dpre_b != nullptr : p == P_GATE ? a.dgate != nullptr
                               : p == P_POST_W ? a.dpost_w != nullptr : a.dpost_b != nullptr;
-            if (!wanted) continue;
+            const int d = 4 * (64 * W * k + t);
+            if (wanted) store4<VEC>(SC_F32, part, (int64_t)p * D + d, v, D - d);
+        };
+        if (RPB == 1) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (RPB > 1) {
-                    __syncthreads();
-                    if (side > 0) join[(side - 1) * 64 * W + t] = acc[p][k];
-                    __syncthreads();
-                    if (side > 0) continue;
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int o = 0; o < RPB - 1; ++o) acc[p][k] += join[o * 64 * W + t];
-                }
-                const int d = 4 * (64 * W * k + t);
-                store4<VEC>(SC_F32, part, (int64_t)p * D + d, acc[p][k], D - d);
+                for (int k = 0; k < NV; ++k) put(p, k, acc[p][k]);
+        } else {
+            __syncthreads();                        // (the last batch entry's have been read)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int k = 0; k < NV; ++k) join[side][p * NV + k][t] = acc[p][k];
+            __syncthreads();
+            for (int x = side; x < NP * NV; x += RPB) {
+                f4 v = join[0][x][t];
+#pragma unroll
+                for (int o = 1; o < RPB; ++o) v += join[o][x][t];
+                put(x / NV, x % NV, v);
             }
         }
     }

@@ -22,19 +22,26 @@ struct RopeArgs {
 // (1 / 2 pi is one, and so is its product with freq), so that cutting it to [-1/2, 1/2] loses nothing at any position.
 __device__ __forceinline__ void turns(const RopeArgs &a, int b, int64_t token, int p0, f4 &c, f4 &s) {
     constexpr double INV_HI = 0x1.45f306dc9c883p-3, INV_LO = -0x1.6b01ec5417056p-57;
+    // (all loads before any use; what is not there is read where it does no harm and does not turn)
+    int ax[4];
+    double f[4];
+    int32_t pos[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int p = p0 + j;
-        double n = 0.0;
-        if (p < a.d.pairs) {
-            const int ax = a.axis[p];
-            if ((unsigned)ax < (unsigned)a.d.axes) {
-                const double f = a.freq[p], pos = (double)a.pos[(int64_t)b * a.d.stridePB + (int64_t)ax * a.d.stridePA + token];
-                const double step = f * INV_HI, rest = fma(f, INV_HI, -step) + f * INV_LO;
-                const double whole = pos * step;
-                n = (whole - rint(whole)) + (fma(pos, step, -whole) + pos * rest);
-            }
-        }
+        const int p = min(p0 + j, a.d.pairs - 1);
+        ax[j] = a.axis[p];
+        f[j] = a.freq[p];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool there = (unsigned)ax[j] < (unsigned)a.d.axes;
+        pos[j] = a.pos[(int64_t)b * a.d.stridePB + (int64_t)(there ? ax[j] : 0) * a.d.stridePA + token];
+        if (!there) f[j] = 0.0;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double x = (double)pos[j], step = f[j] * INV_HI, rest = fma(f[j], INV_HI, -step) + f[j] * INV_LO, whole = x * step;
+        const double n = (whole - rint(whole)) + (fma(x, step, -whole) + x * rest);
         float si, co;
         sincospif((float)(2.0 * n), &si, &co);
         c[j] = co;
@@ -73,7 +80,7 @@ struct Eight {
 // HEADS of them at a time, the next ones' loads in flight.  Memory-bound.  VEC: rows, pairs and halves on four elements.
 // STREAM: stores that do not stay in the caches.
 constexpr int HEADS = 4;
-template <bool VEC, bool NEAR, int R, bool STREAM>
+template <bool VEC, bool NEAR, int R, bool STREAM, bool INT8>
 __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int shift) {
     const sc_rope_desc &d = a.d;
     if (block_id() >= blocks) return;
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int s
             }
             const int64_t at = to + (int64_t)(first + h) * d.strideOH;
             const int k0 = first + h < h1 ? n0 : 0, k1 = first + h < h1 ? n1 : 0;
-            if (d.typeO == SC_INT8) {
+            if (INT8) {
                 float m = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -183,10 +190,16 @@ static bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, in
     return true;
 }
 
-template <bool VEC, int R, bool STREAM>
+template <bool VEC, int R, bool STREAM, bool INT8>
 static void launch_rope(const RopeArgs &a, bool near, dim3 grid, uint32_t blocks, int shift, hipStream_t st) {
-    if (near) hipLaunchKernelGGL((k_rope<VEC, true, R, STREAM>), grid, dim3(256), 0, st, a, blocks, shift);
-    else hipLaunchKernelGGL((k_rope<VEC, false, R, STREAM>), grid, dim3(256), 0, st, a, blocks, shift);
+    if (near) hipLaunchKernelGGL((k_rope<VEC, true, R, STREAM, INT8>), grid, dim3(256), 0, st, a, blocks, shift);
+    else hipLaunchKernelGGL((k_rope<VEC, false, R, STREAM, INT8>), grid, dim3(256), 0, st, a, blocks, shift);
+}
+template <bool VEC, int R>
+static void launch_rope(const RopeArgs &a, bool near, bool past, dim3 grid, uint32_t blocks, int shift, hipStream_t st) {
+    if (a.d.typeO == SC_INT8) launch_rope<VEC, R, false, true>(a, near, grid, blocks, shift, st);
+    else if (VEC && past) launch_rope<VEC, R, VEC, false>(a, near, grid, blocks, shift, st);
+    else launch_rope<VEC, R, false, false>(a, near, grid, blocks, shift, st);
 }
 
 }  // namespace scl
@@ -249,16 +262,9 @@ extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *p
     // 24960 x 24 x 128 in 16 bits 74 -> 62 us.  One that they hold is not: 8192 x 8 x 256 in 32 bits takes 26 us either way, and
     // its reader finds it there.
     const bool stream_past = (int64_t)d.batch * d.tokens * d.heads * d.D * type_bytes(d.typeO) > (int64_t)128 << 20;
-    if (vec && wide) {
-        if (stream_past) launch_rope<true, 4, true>(a, near, grid, n, shift, st);
-        else launch_rope<true, 4, false>(a, near, grid, n, shift, st);
-    } else if (vec) {
-        if (stream_past) launch_rope<true, 2, true>(a, near, grid, n, shift, st);
-        else launch_rope<true, 2, false>(a, near, grid, n, shift, st);
-    } else if (wide) {
-        launch_rope<false, 4, false>(a, near, grid, n, shift, st);
-    } else {
-        launch_rope<false, 2, false>(a, near, grid, n, shift, st);
-    }
+    if (vec && wide) launch_rope<true, 4>(a, near, stream_past, grid, n, shift, st);
+    else if (vec) launch_rope<true, 2>(a, near, stream_past, grid, n, shift, st);
+    else if (wide) launch_rope<false, 4>(a, near, stream_past, grid, n, shift, st);
+    else launch_rope<false, 2>(a, near, stream_past, grid, n, shift, st);
     return hipGetLastError() == hipSuccess ? SC_OK : SC_ERR_HIP;
 }
