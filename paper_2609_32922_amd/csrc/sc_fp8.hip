@@ -490,12 +490,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(Gemm
     };
     const auto copy = [&](int buf, int k) { copy16(from, off[k], lds_address(&sm[buf][(wave * CH + k) * 64])); };
     const auto copy_scales = [&](int buf) { copy4(sfrom, soff, lds_address(&sc[buf][wave * WR])); };
-    enter();
-    if (g.KB > 0) {
-#pragma unroll
-        for (int k = 0; k < CH; ++k) copy(0, k);
-        copy_scales(0);
+    // Where some blocks have a tile less than others, those start a part of a tile later (two sleeps, 7 us; the shortest
+    // tile takes that): else the whole chip stores its outputs at the same time, and multiplies nothing meanwhile
+    // (18464 x 4096 x 1024: 124 us at once, 113 with one sleep, 101 with two, 101 with three).
+    if (const uint32_t more = tiles % gridDim.x; ALONE && tiles > gridDim.x && more != 0 && blockIdx.x >= more) {
+        __builtin_amdgcn_s_sleep(127);
+        __builtin_amdgcn_s_sleep(127);
     }
+    enter();
+#pragma unroll
+    for (int k = 0; k < CH; ++k) copy(0, k);
+    copy_scales(0);
     const int cut = g.K & 127;
     int buf = 0;
     for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
@@ -571,10 +576,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(Gemm
 #pragma unroll
                 for (int j = 0; j < NI; ++j) add(MI - 1, j);
             buf ^= 1;
-        }
-        if (g.KB == 0) {
-            next += gridDim.x;
-            if (next < tiles) enter();
         }
         store_tile<EXACT, true>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
     }
@@ -809,12 +810,13 @@ __global__ __launch_bounds__(256) void k_fp8_lay(const uint8_t *src, int64_t ld,
 
 // How a product is done.  Tiles of 128 x 128 (two blocks to a compute unit) or, for 16-bit results, 256 x 256 (one) where there
 // are enough for half of the compute units; their operands have to lie on 16 bytes, or are laid out so first.  Few tiles:
-// 64 x 64 by groups of waves.  Up to 16 rows: without LDS.
+// 64 x 64 by groups of waves (so too K = 0, a product of the bias alone).  Up to 16 rows: without LDS.
 enum { DIRECT, PARTS, TILES };
 static int64_t tiles_of(const GemmArgs &g, int side) { return ((int64_t)g.M + side - 1) / side * (((int64_t)g.N + side - 1) / side) * g.batch; }
 static bool rows_aligned(int64_t ld, int64_t stride, int batch) { return ld % 16 == 0 && (batch == 1 || stride % 16 == 0); }
 static int way_of(const GemmArgs &g) {
-    if (g.M <= 16 || g.KB == 0) return DIRECT;
+    if (g.M <= 16) return DIRECT;
+    if (g.KB == 0) return PARTS;
     const int64_t tiles = tiles_of(g, 128);
     // (copies to LDS and a tile's scales have 32-bit offsets)
     return tiles < 128 || tiles > INT32_MAX / 4 || g.ldsA > 1 << 21 || g.ldsB > 1 << 21 ? PARTS : TILES;
@@ -852,7 +854,7 @@ static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
         else launch_parts<TA, TB, EXACT, 2>(g, st);
     } else {
         // Microseconds by what was measured: a stage of a round of tiles and what a round costs besides (8192 x 8192 x 8192 takes
-        // 517 us in 256 x 256 tiles and 628 in 128 x 128; 4096 x 4608 x 1152 51 and 40; 18464 x 4096 x 1024 109 and 110).
+        // 517 us in 256 x 256 tiles and 628 in 128 x 128; 4096 x 4608 x 1152 51 and 40; 18464 x 4096 x 1024 101 and 114).
         const double big = (double)((tiles_of(g, 256) + 255) / 256) * (2.0 * g.KB + 5.6),
                      small = (double)((tiles_of(g, 128) + 511) / 512) * (1.225 * g.KB + 1.2);
         if (EXACT || small < big) {

@@ -153,6 +153,9 @@ GEMM = [
     (16, 577, 577, 64, E4, E4, 1, 1, F32, False, False),
     (12, 197, 64, 197, E4, E4, 1, 1, F32, True, False),
     (2, 700, 900, 260, E4, E4, 128, 128, F32, True, False),
+    (1, 16000, 2040, 1000, E4, E4, 1, 128, BF16, True, True),
+    (1, 8000, 4000, 1016, E5, E4, 1, 1, F16, False, True),
+    (2, 5000, 3000, 1024, E4, E4, 128, 1, BF16, True, False),
 ]
 
 
@@ -239,6 +242,12 @@ def test_fp8_gemm_empty(scg):
     out = scg.fp8_gemm(z(3, 0, device="cuda").to(E4), z(3, 0, device="cuda"), z(7, 0, device="cuda").to(E4), z(7, 0, device="cuda"),
                        bias=b, out_dtype=F32)
     assert torch.equal(out, b.expand(3, 7))
+    b = torch.arange(700.0, device="cuda")
+    for M in (17, 3000):
+        for to in (F32, BF16):
+            out = scg.fp8_gemm(z(M, 0, device="cuda").to(E4), z(M, 0, device="cuda"), z(700, 0, device="cuda").to(E4),
+                               z(6, 0, device="cuda"), bias=b, out_dtype=to)
+            assert torch.equal(out, b.to(to).expand(M, 700))
 
 
 def test_offsets_past_32_bits(scg):
