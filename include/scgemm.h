@@ -372,7 +372,7 @@ int sc_residual_norm_backward(const sc_norm_desc *desc, const void *xo, const vo
 enum { SC_ROPE_HALVES = 0, SC_ROPE_NEIGHBOURS = 1 };
 
 typedef struct sc_rope_desc {
-    int32_t batch, tokens, heads, D;   /* x[b] is tokens x heads x D; D <= SC_ROPE_D_LIMIT */
+    int32_t batch, tokens, heads, D;   /* x[b] is tokens x heads x D; heads <= 2^30, D <= SC_ROPE_D_LIMIT */
     int32_t pairs, axes;        /* the first 2 * pairs elements turn (2 * pairs <= D); 1..SC_ROPE_AXES_LIMIT axes */
     int32_t pairing;            /* SC_ROPE_HALVES: pair p is elements p and pairs + p; SC_ROPE_NEIGHBOURS: 2p and 2p + 1 */
     int32_t inverse;            /* 0, or 1: turn back (the gradient) */

@@ -809,7 +809,7 @@ __global__ __launch_bounds__(256) void k_fp8_lay(const uint8_t *src, int64_t ld,
 }
 
 // How a product is done.  Tiles of 128 x 128 (two blocks to a compute unit) or, for 16-bit results, 256 x 256 (one) where there
-// are enough for half of the compute units; their operands have to lie on 16 bytes, or are laid out so first.  Few tiles:
+// are enough for half of the compute units; their rows have to start 16 bytes apart, or are laid out so first.  Few tiles, or an address off 16:
 // 64 x 64 by groups of waves (so too K = 0, a product of the bias alone).  Up to 16 rows: without LDS.
 enum { DIRECT, PARTS, TILES };
 static int64_t tiles_of(const GemmArgs &g, int side) { return ((int64_t)g.M + side - 1) / side * (((int64_t)g.N + side - 1) / side) * g.batch; }

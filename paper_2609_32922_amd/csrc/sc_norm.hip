@@ -590,9 +590,9 @@ static void backward_of(const NormArgs &a, int types, hipStream_t st) {
     else if (types == ANY_16) launch_backward<W, NV, 4, 2, true>(a, st);
     else launch_backward<W, NV, 4, 4, true>(a, st);
 }
-// Forward: the fewest waves that hold a row in five quads a thread (four from 1280 elements on).  Backward: two (three)
-// quads, whose sums leave registers for the next row.  Rows that are read element by element (an odd length or
-// alignment) have two sizes only.
+// The fewest waves that hold a row in two quads a thread (three just below a power of two's half); backward from 4096
+// elements on four, as more waves would wait for each other more.  Rows that are read element by element (an odd length or
+// alignment) have four sizes.
 static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_t st) {
     const bool x16 = a.typeX != SC_F32, rest16 = (a.y == nullptr || a.typeY != SC_F32) && a.typeP != SC_F32 && (!back || a.dh == nullptr || a.typeH != SC_F32);
     const int types = x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;

@@ -112,58 +112,58 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int s
             for (int h = 0; h < HEADS; ++h) x[h] = next[h];
             load(first + HEADS);
 #pragma unroll
-          for (int h = 0; h < HEADS; ++h) {
-            const f4 u = x[h].quad(d.typeX, 0), v = x[h].quad(d.typeX, 1);
-            f4 o0 = u, o1 = v;
-            if (turn) {
-                if (NEAR) {
-                    o0 = f4{u[0] * c[0] - u[1] * s[0], u[0] * s[0] + u[1] * c[0], u[2] * c[1] - u[3] * s[1], u[2] * s[1] + u[3] * c[1]};
-                    o1 = f4{v[0] * c[2] - v[1] * s[2], v[0] * s[2] + v[1] * c[2], v[2] * c[3] - v[3] * s[3], v[2] * s[3] + v[3] * c[3]};
-                } else {
+            for (int h = 0; h < HEADS; ++h) {
+                const f4 u = x[h].quad(d.typeX, 0), v = x[h].quad(d.typeX, 1);
+                f4 o0 = u, o1 = v;
+                if (turn) {
+                    if (NEAR) {
+                        o0 = f4{u[0] * c[0] - u[1] * s[0], u[0] * s[0] + u[1] * c[0], u[2] * c[1] - u[3] * s[1], u[2] * s[1] + u[3] * c[1]};
+                        o1 = f4{v[0] * c[2] - v[1] * s[2], v[0] * s[2] + v[1] * c[2], v[2] * c[3] - v[3] * s[3], v[2] * s[3] + v[3] * c[3]};
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        o0[j] = u[j] * c[j] - v[j] * s[j];
-                        o1[j] = u[j] * s[j] + v[j] * c[j];
+                        for (int j = 0; j < 4; ++j) {
+                            o0[j] = u[j] * c[j] - v[j] * s[j];
+                            o1[j] = u[j] * s[j] + v[j] * c[j];
+                        }
                     }
                 }
-            }
-            const int64_t at = to + (int64_t)(first + h) * d.strideOH;
-            const int k0 = first + h < h1 ? n0 : 0, k1 = first + h < h1 ? n1 : 0;
-            if (INT8) {
-                float m = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j < k0) m = fmaxf(m, fabsf(o0[j]));
-                    if (j < k1) m = fmaxf(m, fabsf(o1[j]));
-                }
-                for (int o = G / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-                const float sc = m / 127.0f;
-                if (live && sub == 0 && first + h < h1) {
-                    const int64_t si = (int64_t)b * d.strideSB + token * d.strideST + (int64_t)(first + h) * d.strideSH;
-                    a.scale[si] = sc;
-                    if (a.rowmax) a.rowmax[si] = m;
-                }
-                store_bytes4<VEC>(a.out, at + e0, quant_int8x4(o0, sc), k0);
-                store_bytes4<VEC>(a.out, at + e1, quant_int8x4(o1, sc), k1);
-            } else if (VEC && NEAR && d.typeO != SC_F32) {
-                if (k1 > 0) {
-                    u4 w;
+                const int64_t at = to + (int64_t)(first + h) * d.strideOH;
+                const int k0 = first + h < h1 ? n0 : 0, k1 = first + h < h1 ? n1 : 0;
+                if (INT8) {
+                    float m = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float lo = j < 2 ? o0[2 * (j & 1)] : o1[2 * (j & 1)], hi = j < 2 ? o0[2 * (j & 1) + 1] : o1[2 * (j & 1) + 1];
-                        w[j] = to_pair(d.typeO, lo, hi);
+                        if (j < k0) m = fmaxf(m, fabsf(o0[j]));
+                        if (j < k1) m = fmaxf(m, fabsf(o1[j]));
                     }
-                    u4_8 *q = reinterpret_cast<u4_8 *>(static_cast<uint16_t *>(a.out) + at + e0);
-                    if (STREAM) __builtin_nontemporal_store(w, q);
-                    else *q = w;
+                    for (int o = G / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+                    const float sc = m / 127.0f;
+                    if (live && sub == 0 && first + h < h1) {
+                        const int64_t si = (int64_t)b * d.strideSB + token * d.strideST + (int64_t)(first + h) * d.strideSH;
+                        a.scale[si] = sc;
+                        if (a.rowmax) a.rowmax[si] = m;
+                    }
+                    store_bytes4<VEC>(a.out, at + e0, quant_int8x4(o0, sc), k0);
+                    store_bytes4<VEC>(a.out, at + e1, quant_int8x4(o1, sc), k1);
+                } else if (VEC && NEAR && d.typeO != SC_F32) {
+                    if (k1 > 0) {
+                        u4 w;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float lo = j < 2 ? o0[2 * (j & 1)] : o1[2 * (j & 1)], hi = j < 2 ? o0[2 * (j & 1) + 1] : o1[2 * (j & 1) + 1];
+                            w[j] = to_pair(d.typeO, lo, hi);
+                        }
+                        u4_8 *q = reinterpret_cast<u4_8 *>(static_cast<uint16_t *>(a.out) + at + e0);
+                        if (STREAM) __builtin_nontemporal_store(w, q);
+                        else *q = w;
+                    } else {
+                        store4<VEC, STREAM>(d.typeO, a.out, at + e0, o0, k0);
+                    }
                 } else {
                     store4<VEC, STREAM>(d.typeO, a.out, at + e0, o0, k0);
+                    store4<VEC, STREAM>(d.typeO, a.out, at + e1, o1, k1);
                 }
-            } else {
-                store4<VEC, STREAM>(d.typeO, a.out, at + e0, o0, k0);
-                store4<VEC, STREAM>(d.typeO, a.out, at + e1, o1, k1);
             }
-          }
         }
     }
 }
@@ -212,7 +212,7 @@ extern "C" int sc_rope(const sc_rope_desc *desc, const void *x, const int32_t *p
     const sc_rope_desc &d = *desc;
     if (d.reserved[0] != 0 || d.reserved[1] != 0) return SC_ERR_RESERVED;
     if (d.batch < 0 || d.tokens < 0 || d.heads < 0 || d.D < 0 || d.D > SC_ROPE_D_LIMIT || d.pairs < 0 || 2 * (int64_t)d.pairs > d.D ||
-        d.axes < 1 || d.axes > SC_ROPE_AXES_LIMIT)
+        d.axes < 1 || d.axes > SC_ROPE_AXES_LIMIT || d.heads > 1 << 30)
         return SC_ERR_SHAPE;
     if (!is_float_type(d.typeX) || (!is_float_type(d.typeO) && d.typeO != SC_INT8)) return SC_ERR_TYPE;
     if ((d.pairing != SC_ROPE_HALVES && d.pairing != SC_ROPE_NEIGHBOURS) || (d.inverse != 0 && d.inverse != 1)) return SC_ERR_TYPE;

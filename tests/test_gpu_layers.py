@@ -493,6 +493,24 @@ def test_residual_norm_backward_forms(scg):
     assert all(bool((none[k] == 0).all()) for k in p) and none["x"].shape == (2, 0, 256)
 
 
+def test_residual_norm_backward_in_place(scg):
+    # dx over dxo, rows side by side and by several waves, four elements at a time and one
+    _note("residual_norm_backward in place")
+    for rows, D in ((701, 256), (530, 1152), (300, 2100), (67, 777)):
+        xo, y, p, gen = _norm_inputs((1, rows, D, BF16, BF16, BF16, F32, 1, 2, ALL, {}), 3)
+        dxo, dh = _randn((1, rows, D), gen, BF16), _randn((1, rows, D), gen, BF16)
+        want = scg.residual_norm_backward(xo, y, dxo=dxo, dh=dh, post=1, pre=2, **{**p, "gate": None})
+        d = scg._lib.ScNormDesc(batch=1, rows=rows, D=D, post=1, pre=2, typeX=1, typeY=1, typeP=0, typeH=1, eps_post=1e-6, eps_pre=1e-6, scale_res=1.0,
+                           ldx=D, ldy=D, ldxo=D, ldh=D, lddxo=D, lddy=D)
+        dy = torch.empty_like(y)
+        w = {k: q.reshape(-1) for k, q in p.items()}
+        assert all(q.numel() == D for q in w.values())
+        rc = scg._lib.sc_residual_norm_backward(d, xo.data_ptr(), y.data_ptr(), w["post_weight"].data_ptr(), w["post_bias"].data_ptr(), 0,
+                                                w["pre_weight"].data_ptr(), dxo.data_ptr(), dh.data_ptr(), dxo.data_ptr(), dy.data_ptr(), 0, 0,
+                                                0, 0, 0, 0, 0, 0)
+        assert rc == 0 and torch.equal(dxo, want["x"]) and torch.equal(dy, want["y"])
+
+
 def test_residual_norm_backward_against_differences(scg):
     """The directional derivative of the kernel's own forward pass in float32.  A central difference of step t is off by
     t^2/6 of the third derivative, taken from differences of steps t and 2t in 64 bits, and by the outputs' errors over t."""
@@ -585,6 +603,13 @@ def test_rope_there_and_back_and_views(scg):
         assert torch.equal(turned, scg.rope(keep[:, :Hq + Hk].contiguous(), pos, freq, axis, interleaved=inter))
         scg.rope(qkv[:, :Hq + Hk], pos, freq, axis, interleaved=inter, out=qkv[:, :Hq + Hk])
         assert torch.equal(qkv[:, :Hq + Hk], turned) and torch.equal(qkv[:, Hq + Hk:], keep[:, Hq + Hk:])
+    # all heads by one thread, and a result that is stored past the caches, over its source
+    far = torch.randint(0, 5000, (3, 9000), generator=gen, device="cuda", dtype=torch.int32)
+    for inter in (False, True):
+        x = _randn((9000, 131, D), gen, BF16)
+        few = scg.rope(x[:300], far[:, :300], freq, axis, interleaved=inter), scg.rope(x[8700:], far[:, 8700:], freq, axis, interleaved=inter)
+        scg.rope(x, far, freq, axis, interleaved=inter, out=x)
+        assert torch.equal(x[:300], few[0]) and torch.equal(x[8700:], few[1])
     # the inverse is the transpose: <rope(x), g> = <x, rope_inverse(g)>
     x, g = _randn((T, Hq, D), gen), _randn((T, Hq, D), gen)
     l = (scg.rope(x, pos, freq, axis).double() * g.double()).sum()

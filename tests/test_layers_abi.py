@@ -189,7 +189,7 @@ def _rope(lib, **kw):
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(batch=-1), "SHAPE"), (dict(tokens=-1), "SHAPE"), (dict(heads=-1), "SHAPE"), (dict(D=258), "SHAPE"), (dict(pairs=33), "SHAPE"), (dict(pairs=-1), "SHAPE"),
+    (dict(batch=-1), "SHAPE"), (dict(tokens=-1), "SHAPE"), (dict(heads=-1), "SHAPE"), (dict(heads=(1 << 30) + 1), "SHAPE"), (dict(D=258), "SHAPE"), (dict(pairs=33), "SHAPE"), (dict(pairs=-1), "SHAPE"),
     (dict(axes=0), "SHAPE"), (dict(axes=9), "SHAPE"), (dict(typeX=5), "TYPE"), (dict(typeO=3), "TYPE"), (dict(pairing=2), "TYPE"),
     (dict(inverse=2), "TYPE"), (dict(reserved=0), "RESERVED"), (dict(reserved=1), "RESERVED"), (dict(strideXT=-1), "STRIDE"),
     (dict(strideOH=63), "STRIDE"), (dict(strideOT=100), "STRIDE"), (dict(strideOB=0), "STRIDE"), (dict(typeO=5, strideSH=9), "STRIDE"),
