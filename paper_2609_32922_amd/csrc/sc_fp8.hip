@@ -36,6 +36,10 @@ struct Raw8 {
             const u4 *q = reinterpret_cast<const u4 *>(static_cast<const uint8_t *>(p) + at * (TX == SC_F32 ? 4 : 2));
 #pragma unroll
             for (int k = 0; k < (TX == SC_F32 ? 2 : 1); ++k) w[k] = q[k];
+        } else if (n >= 8) {
+            const u4_any *q = reinterpret_cast<const u4_any *>(static_cast<const uint8_t *>(p) + at * (TX == SC_F32 ? 4 : 2));
+#pragma unroll
+            for (int k = 0; k < (TX == SC_F32 ? 2 : 1); ++k) w[k] = q[k];
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -90,6 +94,8 @@ __global__ __launch_bounds__(256) void k_fp8_rows(QuantArgs a, uint32_t blocks) 
             uint8_t *q = a.Q + (size_t)b * a.strideQ + (size_t)row[k] * a.ldq + d[k];
             if (VEC) {
                 if (n[k] > 0) *reinterpret_cast<u2 *>(q) = w;
+            } else if (n[k] >= 8) {
+                *reinterpret_cast<u2_any *>(q) = w;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -142,6 +148,8 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(QuantArgs a) {
             uint8_t *q = a.Q + (size_t)b * a.strideQ + min(i, (int64_t)a.rows - 1) * a.ldq + d;
             if (VEC) {
                 if (n > 0) *reinterpret_cast<u2 *>(q) = w;
+            } else if (n >= 8) {
+                *reinterpret_cast<u2_any *>(q) = w;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -156,7 +164,7 @@ __global__ __launch_bounds__(256) void k_fp8_tiles(QuantArgs a) {
 // 15.3 us, 3.7 TB/s).
 constexpr int QT_COLS = 64, QT_LD = 33;      // dwords of a column in LDS: 128 bytes and one to spread the banks
 template <int TX, bool VEC>
-__global__ __launch_bounds__(256) void k_fp8_turned(QuantArgs a, int colblocks, int vecq) {
+__global__ __launch_bounds__(256) void k_fp8_turned(QuantArgs a, int colblocks) {
     __shared__ float part[4][QT_COLS];
     __shared__ uint32_t turned[QT_COLS * QT_LD];
     const float top = a.e5 ? E5M2_MAX : E4M3_MAX;
@@ -204,8 +212,8 @@ __global__ __launch_bounds__(256) void k_fp8_turned(QuantArgs a, int colblocks, 
                 u4 w;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[k] = turned[c * QT_LD + (at >> 2) + k];
-                if (vecq && n == 16) {
-                    *reinterpret_cast<u4 *>(q) = w;
+                if (n == 16) {
+                    *reinterpret_cast<u4_any *>(q) = w;
                 } else {
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
@@ -226,9 +234,8 @@ static hipError_t launch_quant_fp8(const QuantArgs &a, int block, hipStream_t st
         hipLaunchKernelGGL((k_fp8_tiles<TX, VEC>), grid_of(tiles, a.batch), dim3(256), 0, st, a);
     } else {
         const int colblocks = (a.K + QT_COLS - 1) / QT_COLS;
-        const int vecq = aligned_to(a.Q, 16) && a.ldq % 16 == 0 && a.strideQ % 16 == 0;
         hipLaunchKernelGGL((k_fp8_turned<TX, VEC>), grid_of((uint32_t)((int)(((int64_t)a.rows + 127) / 128)) * (uint32_t)colblocks, a.batch), dim3(256), 0,
-                           st, a, colblocks, vecq);
+                           st, a, colblocks);
     }
     return hipGetLastError();
 }

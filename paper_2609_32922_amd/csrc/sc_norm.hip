@@ -76,30 +76,17 @@ struct RawRow {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int at = 16 * (64 * W * k + t);
-                if (VEC) {
-                    const u4 x = __builtin_amdgcn_raw_buffer_load_b128(p, at, 0, 0);
+                const u4 x = __builtin_amdgcn_raw_buffer_load_b128(p, at, 0, 0);
 #pragma unroll
-                    for (int j = 0; j < R; ++j) w[k][j] = x[j];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < R; ++j) w[k][j] = __builtin_amdgcn_raw_buffer_load_b32(p, at + 4 * j, 0, 0);
-                }
+                for (int j = 0; j < R; ++j) w[k][j] = x[j];
             }
         } else {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int at = 8 * (64 * W * k + t);
-                if (VEC) {
-                    const u2 x = __builtin_amdgcn_raw_buffer_load_b64(p, at, 0, 0);
-                    w[k][0] = x[0];
-                    w[k][1] = x[1];
-                } else {
-                    uint32_t h[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) h[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(p, at + 2 * j, 0, 0);
-                    w[k][0] = h[0] | h[1] << 16;
-                    w[k][1] = h[2] | h[3] << 16;
-                }
+                const u2 x = __builtin_amdgcn_raw_buffer_load_b64(p, at, 0, 0);
+                w[k][0] = x[0];
+                w[k][1] = x[1];
             }
         }
     }
@@ -116,8 +103,9 @@ struct RawRow {
 #pragma unroll
                     for (int j = 0; j < R; ++j) w[k][j] = x[j];
                 } else {
+                    const Raw4 x = load_raw<false>(SC_F32, q, d, D - d);
 #pragma unroll
-                    for (int j = 0; j < R; ++j) w[k][j] = d + j < D ? q[d + j] : 0u;
+                    for (int j = 0; j < R; ++j) w[k][j] = x.w[j];
                 }
             }
         } else {
@@ -131,10 +119,9 @@ struct RawRow {
                     w[k][0] = x[0];
                     w[k][1] = x[1];
                 } else {
-                    w[k][0] = w[k][1] = 0u;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (d + j < D) w[k][j >> 1] |= (uint32_t)q[d + j] << (16 * (j & 1));
+                    const Raw4 x = load_raw<false>(SC_BF16, q, d, D - d);
+                    w[k][0] = x.w[0];
+                    w[k][1] = x.w[1];
                 }
             }
         }
@@ -166,7 +153,9 @@ struct Param {
         if (p) r.load(type, p, at, t, D);
     }
     __device__ __forceinline__ void load_row(int type, const void *p, int b, int64_t stride, int t, int D) {
-        if (p) r.load(type, row_of(p, type, b, stride, 0, 0, D), t);
+        if (!p) return;
+        if (VEC) r.load(type, row_of(p, type, b, stride, 0, 0, D), t);
+        else r.load(type, p, b * stride, t, D);
     }
     // plus `off`, or `none` where there is no parameter
     __device__ __forceinline__ void get(f4 (&v)[NV], int type, const void *p, float off, float none) const {
@@ -180,18 +169,13 @@ struct Param {
         for (int k = 0; k < NV; ++k) v[k] += off;
     }
 };
-template <int W, int NV, bool VEC>
+template <int W, int NV>
 __device__ __forceinline__ void store_row(int type, Buffer p, int t, const f4 (&v)[NV]) {
     if (type == SC_F32) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = 16 * (64 * W * k + t);
-            if (VEC) {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v[k]), p, at, 0, 0);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[k][j]), p, at + 4 * j, 0, 0);
-            }
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v[k]), p, at, 0, 0);
         }
     } else {
         u2 w[NV];
@@ -205,12 +189,7 @@ __device__ __forceinline__ void store_row(int type, Buffer p, int t, const f4 (&
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = 8 * (64 * W * k + t);
-            if (VEC) {
-                __builtin_amdgcn_raw_buffer_store_b64(w[k], p, at, 0, 0);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[k][j >> 1] >> (16 * (j & 1))), p, at + 2 * j, 0, 0);
-            }
+            __builtin_amdgcn_raw_buffer_store_b64(w[k], p, at, 0, 0);
         }
     }
 }
@@ -406,10 +385,18 @@ __global__ __launch_bounds__((Waves<W, BACK_WAVES<W, NV>>::THREADS), W <= 8 ? 2 
         // (a row that is not there is one of zeros)
         const auto fetch = [&](int64_t i) {
             const bool live = i < i1;
-            rx.load(a.typeX, row_of(a.x, a.typeX, b, a.strideXO, i, a.ldxo, D, live), t);
-            rh.load(a.typeH, row_of(a.dh, a.typeH, b, a.strideH, i, a.ldh, D, live), t);
-            ry.load(a.typeY, row_of(a.y, a.typeY, b, a.strideY, i, a.ldy, D, live), t);
-            rg.load(a.typeX, row_of(a.dxo, a.typeX, b, a.strideDXO, i, a.lddxo, D, live), t);
+            const auto get = [&](auto &r, int type, const void *p, int64_t stride, int64_t ld) {
+                if (VEC) r.load(type, row_of(p, type, b, stride, i, ld, D, live), t);
+                else r.load(type, p, b * stride + i * ld, t, p != nullptr && live ? D : 0);
+            };
+            get(rx, a.typeX, a.x, a.strideXO, a.ldxo);
+            get(rh, a.typeH, a.dh, a.strideH, a.ldh);
+            get(ry, a.typeY, a.y, a.strideY, a.ldy);
+            get(rg, a.typeX, a.dxo, a.strideDXO, a.lddxo);
+        };
+        const auto put_row = [&](int type, void *p, int64_t stride, int64_t i, int64_t ld, const f4 (&v)[NV]) {
+            if (VEC) store_row<W, NV>(type, row_of(p, type, b, stride, i, ld, D, i < i1), t, v);
+            else store_row<W, NV, false>(type, p, b * stride + i * ld, t, i < i1 ? D : 0, v);
         };
         fetch(i0 + side);
         // (the parameters are the same for all of the rows)
@@ -472,7 +459,7 @@ __global__ __launch_bounds__((Waves<W, BACK_WAVES<W, NV>>::THREADS), W <= 8 ? 2 
             if (a.dx) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k) e[k] = a.scale_res * g[k];
-                store_row<W, NV, VEC>(a.typeX, row_of(a.dx, a.typeX, b, a.strideX, i, a.ldx, D, live), t, e);
+                put_row(a.typeX, a.dx, a.strideX, i, a.ldx, e);
             }
             if (a.y == nullptr && a.dy == nullptr) continue;
             gate.get(e, a.typeP, a.gate, 0.0f, 1.0f);
@@ -507,7 +494,7 @@ __global__ __launch_bounds__((Waves<W, BACK_WAVES<W, NV>>::THREADS), W <= 8 ? 2 
                         g[k][j] *= e[k][j];
                     }
             }
-            if (a.dy) store_row<W, NV, VEC>(a.typeY, row_of(a.dy, a.typeY, b, a.strideDY, i, a.lddy, D, live), t, g);
+            if (a.dy) put_row(a.typeY, a.dy, a.strideDY, i, a.lddy, g);
         }
         if (a.part == nullptr) continue;
         // The rows side by side join their sums in LDS, each side the ones of every RPB-th quad
@@ -570,7 +557,7 @@ __global__ __launch_bounds__(COLS * GROUPS) void k_norm_sums(NormArgs a) {
 // ----------------------------------------------------------------------------
 // host
 // ----------------------------------------------------------------------------
-enum { ANY_ANY, ANY_16, ALL_16 };     // types of the residual stream, and of the rest
+enum { ODD, ANY_ANY, ANY_16, ALL_16 };     // rows that do not lie on four elements; else types of the residual stream, and of the rest
 
 template <int W, int NV, int RX, int RY, bool VEC>
 static void launch_forward(const NormArgs &a, hipStream_t st) {
@@ -587,31 +574,22 @@ template <int W, int NV>
 static void forward_of(const NormArgs &a, int types, hipStream_t st) {
     if (types == ALL_16) launch_forward<W, NV, 2, 2, true>(a, st);
     else if (types == ANY_16) launch_forward<W, NV, 4, 2, true>(a, st);
-    else launch_forward<W, NV, 4, 4, true>(a, st);
+    else if (types == ANY_ANY) launch_forward<W, NV, 4, 4, true>(a, st);
+    else launch_forward<W, NV, 4, 4, false>(a, st);
 }
 template <int W, int NV>
 static void backward_of(const NormArgs &a, int types, hipStream_t st) {
     if (types == ALL_16) launch_backward<W, NV, 2, 2, true>(a, st);
     else if (types == ANY_16) launch_backward<W, NV, 4, 2, true>(a, st);
-    else launch_backward<W, NV, 4, 4, true>(a, st);
+    else if (types == ANY_ANY) launch_backward<W, NV, 4, 4, true>(a, st);
+    else launch_backward<W, NV, 4, 4, false>(a, st);
 }
-// The fewest waves that hold a row in two quads a thread (three just below a power of two's half); backward from 4096
-// elements on four, as more waves would wait for each other more.  Rows that are read element by element (an odd length or
-// alignment) have four sizes.
+// The fewest waves that hold a row in two quads a thread (three just below a power of two's half); gradients of more than 4096
+// elements in four, since sixteen waves have 128 registers each and spill (1024 x 8192 with both norms: 197 us, and 72 by eight)
 static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_t st) {
     const bool x16 = a.typeX != SC_F32, rest16 = (a.y == nullptr || a.typeY != SC_F32) && a.typeP != SC_F32 && (!back || a.dh == nullptr || a.typeH != SC_F32);
-    const int types = x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;
-    if (!vec && back) {
-        if (D <= 512) launch_backward<1, 2, 4, 4, false>(a, st);
-        else if (D <= 1536) launch_backward<2, 3, 4, 4, false>(a, st);
-        else if (D <= 4096) launch_backward<8, 2, 4, 4, false>(a, st);
-        else launch_backward<16, 4, 4, 4, false>(a, st);
-    } else if (!vec) {
-        if (D <= 768) launch_forward<1, 3, 4, 4, false>(a, st);
-        else if (D <= 1536) launch_forward<2, 3, 4, 4, false>(a, st);
-        else if (D <= 4096) launch_forward<8, 2, 4, 4, false>(a, st);
-        else launch_forward<16, 4, 4, 4, false>(a, st);
-    } else if (back) {
+    const int types = !vec ? ODD : x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;
+    if (back) {
         if (D <= 512) backward_of<1, 2>(a, types, st);
         else if (D <= 1024) backward_of<2, 2>(a, types, st);
         else if (D <= 1536) backward_of<2, 3>(a, types, st);
