@@ -252,6 +252,8 @@ struct GemmArgs {
     int shiftA, shiftB;          // log2 of the rows that share a scale
     int typeO, whole;            // whole: output rows of whole 16-byte stores, at 32-bit offsets in a tile
     int tilesM, tilesN, batch;
+    int parts;                   // blocks that share a tile's stages
+    float *part;                 // their sums [parts][batch][M][N], where there is more than one
 };
 
 // D = X Y^T over 128 elements: lane l holds 32 bytes of X's row l % 16 and of Y's row l % 16, the same
@@ -700,7 +702,8 @@ __global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t til
 
 // Too few tiles for every compute unit, or operands off 16 bytes: a block has 64 x 64 outputs, and KG groups of four waves
 // take every KG-th block of 128 each, through registers (which take any alignment) into two stages of LDS of their own, the
-// next block's loads in flight while one is multiplied; the groups' sums are joined in LDS in order.  Bound by latency
+// next block's loads in flight while one is multiplied; the groups' sums are joined in LDS in order.  Where tiles are few and K is
+// long, g.parts blocks share a tile's stages and k_fp8_join adds their sums.  Bound by latency, about 0.8 us a stage
 // (577 x 1000 x 1031 to float32: 10.4 us).
 template <int TA, int TB, bool EXACT, int KG>
 __global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t tiles) {
@@ -709,8 +712,16 @@ __global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t til
     __shared__ float sc[KG][2][2 * T];
     const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6,
               l16 = lane & 15, q4 = lane >> 4, wm = 32 * (wave & 1), wn = 32 * (wave >> 1);
-    if (block_id() >= tiles) return;
-    const int64_t m0 = (int64_t)(block_id() % (uint32_t)g.tilesM) * T, n0 = (int64_t)(block_id() / (uint32_t)g.tilesM) * T;
+    uint32_t tile = block_id(), part = 0;
+    int t0 = 0, t1 = g.KB;
+    if (g.parts > 1) {
+        part = tile / tiles;
+        tile -= part * tiles;
+        t0 = (int)(part * (uint32_t)g.KB / (uint32_t)g.parts);
+        t1 = (int)((part + 1) * (uint32_t)g.KB / (uint32_t)g.parts);
+    }
+    if (tile >= tiles || part >= (uint32_t)g.parts) return;
+    const int64_t m0 = (int64_t)(tile % (uint32_t)g.tilesM) * T, n0 = (int64_t)(tile / (uint32_t)g.tilesM) * T;
     for (int b = blockIdx.z; b < g.batch; b += gridDim.z) {
         const uint8_t *row[G];
 #pragma unroll
@@ -738,16 +749,16 @@ __global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t til
             if (tid < 2 * T) sc[grp][buf][tid] = s;
         };
         __syncthreads();                             // (the last batch entry's sums have been read)
-        if (grp < g.KB) {
-            load(grp);
+        if (t0 + grp < t1) {
+            load(t0 + grp);
             put(0);
         }
         int buf = 0;
-        for (int t = grp; t - grp < g.KB; t += KG, buf ^= 1) {
+        for (int t = t0 + grp; t - grp < t1; t += KG, buf ^= 1) {
             __syncthreads();
-            const bool more = t + KG < g.KB;
+            const bool more = t + KG < t1;
             if (more) load(t + KG);
-            if (t < g.KB) {
+            if (t < t1) {
                 const u4 *p = sm[grp][buf];
                 const auto read = [&](auto &f, int x) { f.set(p[x * 8 + (q4 ^ swz(x))], p[x * 8 + ((q4 + 4) ^ swz(x))]); };
                 Frag<TB, EXACT> fb[2];
@@ -785,8 +796,27 @@ __global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t til
 #pragma unroll
                 for (int x = 0; x < 4; ++x) acc[x >> 1][x & 1] += join[(w * 4 + x) * 256 + tid];
         }
-        store_tile<EXACT, false>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+        if (g.parts == 1) {
+            store_tile<EXACT, false>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+        } else if (m0 + wm < g.M && n0 + wn < g.N) {
+            const int rows = (int)min(g.M - m0 - wm, (int64_t)32), cols = (int)min(g.N - n0 - wn, (int64_t)32);
+            float *corner = g.part + (((int64_t)part * g.batch + b) * g.M + m0 + wm) * g.N + n0 + wn;
+            store_rows<SC_F32, false, false>(reinterpret_cast<uint8_t *>(corner), nullptr, rows, cols, g.N, l16, q4, acc);
+        }
     }
+}
+// The parts' sums added in order, and the bias: four columns a thread.  Memory-bound.
+__global__ __launch_bounds__(256) void k_fp8_join(GemmArgs g) {
+    const int quads = (g.N + 3) / 4;
+    const int64_t at = (int64_t)block_id() * 256 + threadIdx.x, row = at / quads, entry = (int64_t)g.batch * g.M;
+    if (row >= entry) return;
+    const int n = 4 * (int)(at - row * quads), left = g.N - n;
+    const int64_t b = row / g.M, i = row - b * g.M;
+    f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int k = 0; k < g.parts; ++k) s += to_floats(SC_F32, load_raw<false>(SC_F32, g.part, (k * entry + row) * g.N + n, left));
+    if (g.bias) s += to_floats(SC_F32, load_raw<false>(SC_F32, g.bias, b * g.strideBias + n, left));
+    store4<false>(g.typeO, g.out, b * g.strideO + i * g.ldo + n, s, left);
 }
 
 template <int TA, int TB, bool EXACT, bool BLOCKB, int BM, int BN, int WM, int WN>
@@ -809,7 +839,11 @@ static void launch_parts(GemmArgs g, hipStream_t st) {
     g.tilesM = (int)(((int64_t)g.M + 63) / 64);
     g.tilesN = (int)(((int64_t)g.N + 63) / 64);
     const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN;
-    hipLaunchKernelGGL((k_fp8_parts<TA, TB, EXACT, KG>), grid_of(tiles, g.batch), dim3(256 * KG), 0, st, g, tiles);
+    hipLaunchKernelGGL((k_fp8_parts<TA, TB, EXACT, KG>), grid_of(tiles * (uint32_t)g.parts, g.batch), dim3(256 * KG), 0, st, g, tiles);
+    if (g.parts > 1) {
+        const int64_t quads = (int64_t)g.batch * g.M * ((g.N + 3) / 4);
+        hipLaunchKernelGGL(k_fp8_join, grid_of((uint32_t)((quads + 255) / 256), 1), dim3(256), 0, st, g);
+    }
 }
 // An operand whose rows do not start on 16 bytes, laid out anew: rows of whole blocks of 128, zeros behind K.  Memory-bound,
 // and worth it where many tiles read every row (4608 x 1152 x 4099 to bfloat16: 54 us with it; 39 for 4096, whose rows lie as they
@@ -838,6 +872,19 @@ static int way_of(const GemmArgs &g) {
 }
 static size_t laid_bytes(int rows, int KB, int64_t stride, int batch) {
     return (size_t)rows * KB * 128 * (stride == 0 ? 1 : batch);
+}
+// Blocks that share a tile's stages: one for each compute unit, three stages or more to each of a block's two groups, if that takes
+// ten stages from every group; fewer cost less than the second launch (100 x 1152 x 4608 to bfloat16: 17.4 us alone, 11.6 in six parts;
+// 64 x 256 x 8192 27.3 and 11.3; 256 x 2048 x 8192 30.6 and 22.9; but 17 x 1024 x 2048 9.7 and 11.2 in two).
+static int parts_of(const GemmArgs &g) {
+    const int64_t tiles = tiles_of(g, 64);
+    if (way_of(g) != PARTS || tiles > 128) return 1;
+    const int parts = (int)(256 / tiles < g.KB / 6 ? 256 / tiles : g.KB / 6);
+    return parts > 1 && g.KB * (parts - 1) >= 20 * parts ? parts : 1;
+}
+static size_t part_bytes(const GemmArgs &g) {
+    const int parts = parts_of(g);
+    return parts == 1 ? 0 : (size_t)parts * g.batch * g.M * g.N * sizeof(float);
 }
 // bytes that the operands take that have to be laid out, A's first
 static void lay_sizes(const GemmArgs &g, size_t *a, size_t *b) {
@@ -909,6 +956,7 @@ static GemmArgs gemm_args(const sc_fp8_gemm_desc &d) {
     g.shiftB = d.rowsB == 128 ? 7 : 0;
     g.typeO = d.typeO;
     g.batch = d.batch;
+    g.parts = 1;
     return g;
 }
 
@@ -971,8 +1019,9 @@ int sc_fp8_gemm_workspace_size(const sc_fp8_gemm_desc *desc, size_t *bytes) {
     *bytes = 0;
     if (desc->batch == 0 || desc->M == 0 || desc->N == 0) return SC_OK;
     size_t a, b;
-    lay_sizes(gemm_args(*desc), &a, &b);
-    *bytes = a + b;
+    const GemmArgs g = gemm_args(*desc);
+    lay_sizes(g, &a, &b);
+    *bytes = a + b + part_bytes(g);        // (never both)
     return SC_OK;
 }
 
@@ -1001,6 +1050,8 @@ int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, co
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     if (la > 0 && lay(&g.A, &g.lda, &g.strideA, g.M, g, ws, st) != hipSuccess) return SC_ERR_HIP;
     if (lb > 0 && lay(&g.B, &g.ldb, &g.strideB, g.N, g, ws + la, st) != hipSuccess) return SC_ERR_HIP;
+    g.parts = parts_of(g);
+    if (g.parts > 1) g.part = static_cast<float *>(workspace);
     if (la > 0 && lb > 0) g.K = g.KB * 128;         // (both operands have zeros there now)
     const hipError_t e = d.typeO == SC_F32 ? launch_gemm_types<true>(g, d.typeA, d.typeB, st) : launch_gemm_types<false>(g, d.typeA, d.typeB, st);
     return e == hipSuccess ? SC_OK : SC_ERR_HIP;

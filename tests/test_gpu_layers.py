@@ -153,6 +153,12 @@ GEMM = [
     (16, 577, 577, 64, E4, E4, 1, 1, F32, False, False),
     (12, 197, 64, 197, E4, E4, 1, 1, F32, True, False),
     (2, 700, 900, 260, E4, E4, 128, 128, F32, True, False),
+    # a tile's stages by several blocks
+    (1, 64, 256, 8192, E4, E4, 1, 128, F32, True, True),
+    (1, 290, 383, 7233, E4, E4, 1, 128, F16, False, True),
+    (2, 100, 130, 4099, E5, E4, 1, 1, BF16, True, False),
+    (3, 17, 70, 5000, E4, E5, 128, 1, F32, True, True),
+    (1, 40, 33, 262144, E4, E4, 1, 128, F32, True, True),
     (1, 16000, 2040, 1000, E4, E4, 1, 128, BF16, True, True),
     (1, 8000, 4000, 1016, E5, E4, 1, 1, F16, False, True),
     (2, 5000, 3000, 1024, E4, E4, 128, 1, BF16, True, False),
@@ -196,7 +202,7 @@ def test_fp8_gemm_views(scg):
     _note("fp8_gemm of views")
     gen = _gen(6)
     for off, pad, M, N, K in ((0, 0, 150, 140, 256), (1, 3, 150, 140, 200), (16, 16, 270, 300, 384), (5, 11, 3, 333, 130), (16, 0, 40, 64, 256),
-                               (5, 11, 1500, 1411, 200), (1, 15, 1500, 1411, 240), (16, 16, 1500, 1411, 224)):
+                               (5, 11, 1500, 1411, 200), (1, 15, 1500, 1411, 240), (16, 16, 1500, 1411, 224), (3, 2, 70, 99, 4000), (16, 0, 70, 99, 4000)):
         A0, B0 = (torch.randint(0, 120, (n, K + off + pad), generator=gen, device="cuda", dtype=torch.uint8) for n in (M, N))
         kb = -(-K // 128)
         sA0, sB0 = torch.rand((M, kb + 2), generator=gen, device="cuda"), torch.rand((-(-N // 128), kb + 1), generator=gen, device="cuda")
@@ -214,13 +220,14 @@ def test_fp8_gemm_special_values(scg):
     # NaN and infinities reach their own rows and columns, and nothing else; what lies behind K never counts
     _note("fp8_gemm special values")
     gen = _gen(7)
-    for M, N, K in ((20, 30, 200), (300, 300, 200)):
-        A0 = torch.full((M, 256), 0x7F, dtype=torch.uint8, device="cuda").view(E4)       # NaN behind K
-        B0 = torch.full((N, 256), 0x7F, dtype=torch.uint8, device="cuda").view(E4)
+    for M, N, K in ((20, 30, 200), (300, 300, 200), (40, 30, 200 + 256 * 16)):
+        kb = -(-K // 128)
+        A0 = torch.full((M, 128 * kb), 0x7F, dtype=torch.uint8, device="cuda").view(E4)       # NaN behind K
+        B0 = torch.full((N, 128 * kb), 0x7F, dtype=torch.uint8, device="cuda").view(E4)
         A0[:, :K] = _randn((M, K), gen).to(E4)
         B0[:, :K] = _randn((N, K), gen).to(E4)
         A0[3, 150] = float("nan")
-        sA, sB = torch.ones(M, 2, device="cuda"), torch.ones(N, 2, device="cuda")
+        sA, sB = torch.ones(M, kb, device="cuda"), torch.ones(N, kb, device="cuda")
         sB[5, 1] = float("inf")
         got = scg.fp8_gemm(A0[:, :K], sA, B0[:, :K], sB, out_dtype=F32)
         bad = ~torch.isfinite(got)

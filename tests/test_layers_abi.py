@@ -98,6 +98,13 @@ def test_fp8_gemm_refuses_pointers(lib):
         a = list(ok)
         a[k] = FAKE + 1
         assert lib.sc_fp8_gemm(d, *a, FAKE, 1 << 40, 0) == lib.SC_ERR_STRIDE
+    # sums of blocks that share a tile, and operands laid out anew, lie in the workspace
+    for more in (dict(K=8192, lda=8192, ldb=8192, ldsA=64, ldsB=64), dict(M=4096, N=4096, lda=301, ldo=4096, strideO=1 << 24, strideA=1 << 21)):
+        d = _gemm(lib, **more)
+        need = lib.sc_fp8_gemm_workspace_size(d)
+        assert need > 0
+        for ws, n in ((0, need), (FAKE, need - 1), (FAKE + 16, need)):
+            assert lib.sc_fp8_gemm(d, *ok, ws, n, 0) == lib.SC_ERR_WORKSPACE
     so = lib.load()
     assert so.sc_fp8_gemm_workspace_size(None, ctypes.byref(ctypes.c_size_t())) == lib.SC_ERR_NULL
     assert so.sc_fp8_gemm_workspace_size(ctypes.byref(d), None) == lib.SC_ERR_NULL
