@@ -468,7 +468,8 @@ __global__ __launch_bounds__((Waves<W, BACK_WAVES<W, NV>>::THREADS), W <= 8 ? 2 
                 post_w.get(pw, a.typeP, a.post_w, a.off_post, 1.0f);
                 post_b.get(c, a.typeP, a.post_b, 0.0f, 0.0f);
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+                for (int k = 0; k < NV; ++k) {
+                    const int left = D - 4 * (64 * W * k + t);       // (elements of the row from this quad on)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float nr = m[k][j] * r_post, du = g[k][j] * e[k][j];
@@ -476,8 +477,10 @@ __global__ __launch_bounds__((Waves<W, BACK_WAVES<W, NV>>::THREADS), W <= 8 ? 2 
                         acc[P_GATE][k][j] = fmaf(g[k][j], fmaf(nr, pw[k][j], c[k][j]), acc[P_GATE][k][j]);
                         acc[NP - 2][k][j] = fmaf(du, nr, acc[NP - 2][k][j]);
                         acc[NP - 1][k][j] += du;
-                        g[k][j] = du * pw[k][j];
+                        // (behind the row a LayerNorm's gradient above is - r mean(d), not 0, and must not enter the sums below)
+                        g[k][j] = (VEC ? left > 0 : j < left) ? du * pw[k][j] : 0.0f;
                     }
+                }
                 if (a.dy) {
                     float s[NS] = {dot(g, m), sum(g), 0.0f, 0.0f};
                     sums(s, 2);

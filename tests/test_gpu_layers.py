@@ -485,6 +485,19 @@ def _check_gradients(got, xo, y, p, dxo, dh, post, pre, kw, tx=None):
             _within(g, v, e + R.HALF[t] * (v.abs() + e) + R.LEAST[t], k)
 
 
+@pytest.mark.parametrize("names,kw", [((), {}), (("post_weight", "pre_weight"), dict(post_offset=1.0)), (("post_bias",), {})], ids=["bare", "weights", "bias"])
+@pytest.mark.parametrize("D", [3, 64, 768, 777, 1024, 1152, 1300, 2500, 4100])
+def test_residual_norm_backward_two_layer_norms_without_gate(scg, D, names, kw):
+    # dh with a mean: the pre norm's gradient takes mean(d) off every element, and only off those of the row
+    _note("residual_norm_backward two LayerNorms D=%d %s" % (D, names))
+    for tx, rows in ((F32, 5), (BF16, 19)):
+        case = (2, rows, D, tx, tx, tx, F32, 2, 2, names, kw)
+        xo, y, p, gen = _norm_inputs(case, 4)
+        dxo, dh = _randn((2, rows, D), gen, tx), (_randn((2, rows, D), gen) + 1.5).to(tx)
+        got = scg.residual_norm_backward(xo, y, dxo=dxo, dh=dh, post=2, pre=2, **p, **kw)
+        _check_gradients(got, xo, y, p, dxo, dh, 2, 2, kw)
+
+
 def test_residual_norm_backward_forms(scg):
     # one gradient absent; parameters' gradients not wanted; no branch; many rows and chunks; no rows at all
     _note("residual_norm_backward forms")
