@@ -328,8 +328,9 @@ __device__ __forceinline__ int fragment_row(int l16, int j) { return 16 * (l16 >
 __device__ __forceinline__ int swz_b(int r) { return ((r >> 1) & 1) | ((r >> 3) & 6); }
 
 // Copies 16 (or 4) bytes for each lane from the buffer, at off, to LDS, at `to` (the same in every lane) plus 16 (4)
-// bytes a lane, past the registers.  Nothing waits for it but wait_copies().  What lies behind the buffer's bound
-// leaves no byte of another row in LDS, and only rows that are not stored have any.
+// bytes a lane, past the registers.  Nothing waits for it but wait_copies().  A dword that does not lie whole before the
+// buffer's bound is not loaded (measured: of a last row of 201 bytes under a bound of 201 the last byte was 0; 204 of 204 arrived),
+// so bounds are whole dwords.
 typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ Buffer buffer_of(const void *p, int64_t bytes) {
     const uint64_t x = (uint64_t)p;
@@ -488,7 +489,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(Gemm
     const auto enter = [&]() {
         tile_at(next, tiles, g.tilesM, g.tilesN, &cb, &cm, &cn);
         const int64_t x0 = forB ? (int64_t)cn * BN : (int64_t)cm * BM, rows = min((int64_t)(forB ? BN : BM), all - x0);
-        from = buffer_of(src + cb * stride + x0 * ld, (rows - 1) * ld + g.K);
+        // (up to the end of the dword that holds the last row's last byte; what it holds behind K becomes zero below)
+        from = buffer_of(src + cb * stride + x0 * ld, (rows - 1) * ld + (g.K + 3) / 4 * 4);
         sfrom = buffer_of(ssrc + cb * sstride + (x0 >> shift) * lds, 4 * (((rows - 1) >> shift) * lds + g.KB));
     };
     const auto advance = [&]() {      // to the stage behind the one that has been copied; behind the last there is nothing to read

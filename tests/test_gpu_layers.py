@@ -216,6 +216,26 @@ def test_fp8_gemm_views(scg):
         assert bool((big == -3.0).all())
 
 
+@pytest.mark.parametrize("to", [F32, BF16])
+@pytest.mark.parametrize("M,N,K,ld", [(1500, 1411, 201, 208), (1500, 1411, 203, 256), (1500, 1411, 204, 208), (1500, 1411, 130, 144),
+                                      (1500, 1411, 1031, 1040), (1500, 1411, 127, 128), (5000, 3001, 1029, 1040)])
+def test_fp8_gemm_of_columns_of_padded_rows(scg, M, N, K, ld, to):
+    # rows on 16 bytes whose last elements are no whole 16: these count in every row, a tile's last one too, and what lies behind does not
+    _note("fp8_gemm %d x %d x %d of rows of %d" % (M, N, K, ld))
+    gen = _gen(K)
+    ops = []
+    for n, per in ((M, 1), (N, 128)):
+        x = _randn((n, K), gen)
+        x[:, K - K % 16:] *= 30.0
+        q, s = R.fp8_quantize32(x, E4, per)
+        full = torch.full((n, ld), 0x7F, dtype=torch.uint8, device="cuda").view(E4)       # NaN behind K
+        full[:, :K] = q
+        ops += [full[:, :K], s]
+    got = scg.fp8_gemm(*ops, out_dtype=to)
+    ref, mag = R.fp8_gemm(ops[0], ops[1], 1, ops[2], ops[3], 128)
+    _within(got, ref, R.gemm_tolerance(mag, K, to, ref), "product")
+
+
 def test_fp8_gemm_special_values(scg):
     # NaN and infinities reach their own rows and columns, and nothing else; what lies behind K never counts
     _note("fp8_gemm special values")
