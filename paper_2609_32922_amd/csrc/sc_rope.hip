@@ -42,10 +42,15 @@ __device__ __forceinline__ void turns(const RopeArgs &a, int b, int64_t token, i
     for (int j = 0; j < 4; ++j) {
         const double x = (double)pos[j], step = f[j] * INV_HI, rest = fma(f[j], INV_HI, -step) + f[j] * INV_LO, whole = x * step;
         const double n = (whole - rint(whole)) + (fma(x, step, -whole) + x * rest);
+        // (what rounding the half turns to float32 takes from the angle, up to pi 2^-25, is put back to first order: the square is
+        // below 2^-46.  Beside a cosine or a sine near zero it would be many of its steps.)
+        const double half_turns = 2.0 * n;
+        const float near = (float)half_turns, rest_angle = (float)((half_turns - (double)near) * M_PI);
         float si, co;
-        sincospif((float)(2.0 * n), &si, &co);
-        c[j] = co;
-        s[j] = a.d.inverse ? -si : si;
+        sincospif(near, &si, &co);
+        c[j] = fmaf(-rest_angle, si, co);
+        const float sine = fmaf(rest_angle, co, si);
+        s[j] = a.d.inverse ? -sine : sine;
     }
 }
 

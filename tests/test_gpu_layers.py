@@ -635,6 +635,24 @@ def test_rope(scg, case, shared):
         assert torch.equal(Q.reshape(q.shape), q) and torch.equal(s.reshape(sr.shape), sr) and torch.equal(m.reshape(mr.shape), mr)
 
 
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope_of_unit_vectors(scg, inter, inverse):
+    """(1, 0) turns to the cosine and the sine themselves: each within two steps of float32 (the function) and a rounding, also where
+    one of the two is near zero and a rounding of the angle would be large beside it.  The reference's own angle, below 1000 in 64
+    bits, is off by 2^-43."""
+    _note("rope of unit vectors")
+    freq, axis = scg.rope_table([128])
+    pos = torch.arange(1000, dtype=torch.int32, device="cuda")[None]
+    x = torch.zeros((1000, 2, 128), device="cuda")
+    x[..., slice(0, None, 2) if inter else slice(0, 64)] = 1.0
+    ref, _ = R.rope(x[None], pos[None], freq, axis, inter, inverse)
+    for big in (x, x[:3]):
+        n = big.shape[0]
+        got = scg.rope(big.contiguous(), pos[:, :n], freq, axis, interleaved=inter, inverse=inverse)
+        _within(got[None], ref[:, :n], 6 * R.U * ref[:, :n].abs() + 2.0 ** -41, "turned")
+
+
 def test_rope_there_and_back_and_views(scg):
     _note("rope views")
     gen = _gen(4)
