@@ -197,6 +197,23 @@ def test_fp8_gemm_exact_small_integers(scg):
         assert torch.equal(got.double(), ref)
 
 
+@pytest.mark.parametrize("to", [F32, F16])
+@pytest.mark.parametrize("M,N,K", [(1, 16, 128), (8, 64, 1024), (100, 72, 1024), (64, 256, 8192), (300, 300, 1000), (2000, 1411, 1024), (5000, 3000, 1024)])
+def test_fp8_gemm_small_products_beside_large_ones(scg, M, N, K, to):
+    # of each eight neighbours two products are 2^16 and -2^16 and the others are small: every sum is a whole number that the
+    # result's type holds, so nothing may be lost
+    _note("fp8_gemm small products %d x %d x %d" % (M, N, K))
+    gen = _gen(K + M)
+    a = torch.randint(-2, 3, (M, K), generator=gen, device="cuda").float()
+    b = torch.randint(-2, 3, (N, K), generator=gen, device="cuda").float()
+    a[:, 0::8] = a[:, 1::8] = b[:, 0::8] = 256.0
+    b[:, 1::8] = -256.0
+    one = lambda n: torch.ones(n, -(-K // 128), device="cuda")  # noqa: E731
+    got = scg.fp8_gemm(a.to(E4), one(M), b.to(E4), one(N), out_dtype=to)
+    ref, _ = R.fp8_gemm(a.to(E4), one(M), 1, b.to(E4), one(N), 1)
+    assert float(ref.abs().max()) <= 2048.0 and torch.equal(got.double(), ref)
+
+
 def test_fp8_gemm_views(scg):
     # operands, scales and result inside larger buffers, from odd bytes on; the rest stays as it was
     _note("fp8_gemm of views")
