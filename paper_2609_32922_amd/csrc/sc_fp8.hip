@@ -263,9 +263,9 @@ struct GemmArgs {
 // largest one's power of two (measured: beside a product of 2^16 one of 2^3 counts and one of 2^2 does not) and add the
 // eights in float32.  Seven of eight products may lose up to 2^-13 of the largest each: at most 8.5e-4 of the sum of
 // magnitudes, which is less than a quarter of a bfloat16's half step (3.9e-3) of a result as large as that sum, but more than a
-// float16's (4.9e-4), and more than a rounding of any type where large products cancel.  bfloat16 results take them: operands of
-// random signs up to K = 2^20 come out as near as their rounding lets them (error over the rounding's own 1.000).
-// EXACT, for float32 and float16 results, turns the bytes into float16 (every value of both types is one) and takes the
+// float16's (4.9e-4), and more than a rounding of any type where large products cancel.  bfloat16 results of more than
+// 16 rows take them: operands of random signs up to K = 2^20 come out as near as their rounding lets them (error over the rounding's own 1.000).
+// EXACT, for the others, turns the bytes into float16 (every value of both types is one) and takes the
 // 16-bit products, whose sums are float32 throughout, at half the rate.
 template <int T, bool EXACT>
 struct Frag {
@@ -435,13 +435,14 @@ __device__ __forceinline__ void store_rows(uint8_t *corner, const float *bias, i
         }
     }
 }
-template <bool EXACT, bool RUN, int MI, int NI>
+// (BF, REST: results are bfloat16; float32 and float16)
+template <bool BF, bool REST, bool RUN, int MI, int NI>
 __device__ __forceinline__ void store_tile(const GemmArgs &g, int b, int64_t m0, int64_t n0, int l16, int q4, const f4 (&acc)[MI][NI]) {
     const int rows = (int)min(g.M - m0, (int64_t)(16 * MI)), cols = (int)min(g.N - n0, (int64_t)(16 * NI));
     if (rows <= 0 || cols <= 0) return;
-    uint8_t *corner = static_cast<uint8_t *>(g.out) + (b * g.strideO + m0 * g.ldo + n0) * (EXACT && g.typeO == SC_F32 ? 4 : 2);
+    uint8_t *corner = static_cast<uint8_t *>(g.out) + (b * g.strideO + m0 * g.ldo + n0) * (REST && g.typeO == SC_F32 ? 4 : 2);
     const float *bias = g.bias ? g.bias + b * g.strideBias + n0 : nullptr;
-    if (!EXACT) {
+    if (BF && (!REST || g.typeO == SC_BF16)) {
         if (g.whole) store_rows<SC_BF16, true, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
         else store_rows<SC_BF16, false, RUN>(corner, bias, rows, cols, g.ldo, l16, q4, acc);
     } else if (g.typeO == SC_F32) {
@@ -596,16 +597,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(Gemm
                 for (int j = 0; j < NI; ++j) add(MI - 1, j);
             buf ^= 1;
         }
-        store_tile<EXACT, true>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+        store_tile<!EXACT, EXACT, true>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
     }
 }
 
 // Up to 16 rows: a block has 16 MI x 16 NI outputs, and its eight waves deal the
 // blocks of 128 among themselves.  A wave takes its fragments from memory as they lie (a row's 128 bytes by four lanes, 64 of
-// them at a time), the next block's while one is multiplied; the eight sums are joined in LDS in order.  Bound by latency
-// (1 x 4608 x 1152: 6.2 us).
+// them at a time), the next block's while one is multiplied; the eight sums are joined in LDS in order.  Results of every type
+// take the 16-bit products (Frag): latency bounds it (1 x 4608 x 1152: 6.2 us), and the conversions hide behind it (16 x 4096 x 1024
+// 6.2 us with them and without).
 constexpr int DW = 8;
-template <int TA, int TB, bool EXACT, int MI, int NI>
+template <int TA, int TB, int MI, int NI>
 __global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t tiles) {
     __shared__ f4 join[DW][MI * NI][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q4 = lane >> 4;
@@ -668,12 +670,12 @@ __global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t til
             }
         };
         const auto multiply = [&](const Block &f) {
-            Frag<TB, EXACT> fb[NI];
+            Frag<TB, true> fb[NI];
 #pragma unroll
             for (int j = 0; j < NI; ++j) fb[j].set(f.b[j][0], f.b[j][1]);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                Frag<TA, EXACT> fa;
+                Frag<TA, true> fa;
                 fa.set(f.a[i][0], f.a[i][1]);
 #pragma unroll
                 for (int j = 0; j < NI; ++j) {
@@ -700,7 +702,7 @@ __global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t til
             f4 v[1][1] = {{join[0][x][lane]}};
 #pragma unroll
             for (int w = 1; w < DW; ++w) v[0][0] += join[w][x][lane];
-            store_tile<EXACT, false>(g, b, m0 + 16 * (x / NI), n0 + 16 * (x % NI), l16, q4, v);
+            store_tile<true, true, false>(g, b, m0 + 16 * (x / NI), n0 + 16 * (x % NI), l16, q4, v);
         }
     }
 }
@@ -802,7 +804,7 @@ __global__ __launch_bounds__(256 * KG) void k_fp8_parts(GemmArgs g, uint32_t til
                 for (int x = 0; x < 4; ++x) acc[x >> 1][x & 1] += join[(w * 4 + x) * 256 + tid];
         }
         if (g.parts == 1) {
-            store_tile<EXACT, false>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
+            store_tile<!EXACT, EXACT, false>(g, b, m0 + wm, n0 + wn, l16, q4, acc);
         } else if (m0 + wm < g.M && n0 + wn < g.N) {
             const int rows = (int)min(g.M - m0 - wm, (int64_t)32), cols = (int)min(g.N - n0 - wn, (int64_t)32);
             float *corner = g.part + (((int64_t)part * g.batch + b) * g.M + m0 + wm) * g.N + n0 + wn;
@@ -832,12 +834,12 @@ static void launch_tile(GemmArgs g, int per_cu, hipStream_t st) {
     hipLaunchKernelGGL((k_fp8_gemm<TA, TB, EXACT, BLOCKB, BM, BN, WM, WN>), dim3(tiles < most ? tiles : most), dim3((BM / WM) * (BN / WN) * 64),
                        0, st, g, tiles);
 }
-template <int TA, int TB, bool EXACT, int MI, int NI>
+template <int TA, int TB, int MI, int NI>
 static void launch_direct(GemmArgs g, hipStream_t st) {
     g.tilesM = (int)(((int64_t)g.M + 16 * MI - 1) / (16 * MI));
     g.tilesN = (int)(((int64_t)g.N + 16 * NI - 1) / (16 * NI));
     const uint32_t tiles = (uint32_t)g.tilesM * (uint32_t)g.tilesN;
-    hipLaunchKernelGGL((k_fp8_direct<TA, TB, EXACT, MI, NI>), grid_of(tiles, g.batch), dim3(64 * DW), 0, st, g, tiles);
+    hipLaunchKernelGGL((k_fp8_direct<TA, TB, MI, NI>), grid_of(tiles, g.batch), dim3(64 * DW), 0, st, g, tiles);
 }
 template <int TA, int TB, bool EXACT, int KG>
 static void launch_parts(GemmArgs g, hipStream_t st) {
@@ -913,7 +915,7 @@ static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
     const bool tiled = way_of(g) == TILES && aligned_to(g.A, 16) && aligned_to(g.B, 16) && rows_aligned(g.lda, g.strideA, g.batch) &&
                        rows_aligned(g.ldb, g.strideB, g.batch);
     if (way_of(g) == DIRECT) {
-        launch_direct<TA, TB, EXACT, 1, 1>(g, st);
+        launch_direct<TA, TB, 1, 1>(g, st);
     } else if (!tiled) {
         // one group of waves where there are tiles for all anyway (577 x 4096 x 1024: 16.9 us, 20.5 with two), else two
         // (256 x 4096 x 4096: 23.1 us, 24.2 with one; 577 x 1024 x 4096: 17.9, 23.0)

@@ -208,8 +208,8 @@ def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=Non
     A [M, K] or [batch, M, K], B [N, K] or [batch or 1, N, K] (torch.float8_e4m3fn or float8_e5m2 each); sA float32
     [.., M, ceil(K/128)] or [.., ceil(M/128), ceil(K/128)], sB alike, as ``fp8_quantize`` gives them; bias float32 [N] or
     [batch, N].  ``out_dtype`` (default bfloat16) or ``out`` with rows of any stride.  float32 and float16 results have float32
-    products and sums throughout; bfloat16 ones take the matrix cores' 8-bit products at twice the rate, which may lose up to 7 2^-13 of
-    the sum of the products' magnitudes.  Returns out [.., M, N].
+    products and sums throughout; bfloat16 ones of more than 16 rows take the matrix cores' 8-bit products at twice the rate, which
+    may lose up to 7 2^-13 of the sum of the products' magnitudes.  Returns out [.., M, N].
     """
     import torch
     key = ("gemm", A.shape, A.stride(), A.dtype, A.device, sA.shape, sA.stride(), sA.dtype, sA.device, B.shape, B.stride(), B.dtype,

@@ -197,12 +197,14 @@ def test_fp8_gemm_exact_small_integers(scg):
         assert torch.equal(got.double(), ref)
 
 
-@pytest.mark.parametrize("to", [F32, F16])
+@pytest.mark.parametrize("to", [F32, F16, BF16])
 @pytest.mark.parametrize("M,N,K", [(1, 16, 128), (8, 64, 1024), (100, 72, 1024), (64, 256, 8192), (300, 300, 1000), (2000, 1411, 1024), (5000, 3000, 1024)])
 def test_fp8_gemm_small_products_beside_large_ones(scg, M, N, K, to):
-    # of each eight neighbours two products are 2^16 and -2^16 and the others are small: every sum is a whole number that the
-    # result's type holds, so nothing may be lost
+    # of each eight neighbours two products are 2^16 and -2^16 and the others are small: every sum is a whole number that float32
+    # and float16 hold, so nothing may be lost but its rounding to bfloat16
     _note("fp8_gemm small products %d x %d x %d" % (M, N, K))
+    if to == BF16 and M > 16:
+        pytest.skip("bfloat16 results of more than 16 rows take the 8-bit products")
     gen = _gen(K + M)
     a = torch.randint(-2, 3, (M, K), generator=gen, device="cuda").float()
     b = torch.randint(-2, 3, (N, K), generator=gen, device="cuda").float()
@@ -211,7 +213,7 @@ def test_fp8_gemm_small_products_beside_large_ones(scg, M, N, K, to):
     one = lambda n: torch.ones(n, -(-K // 128), device="cuda")  # noqa: E731
     got = scg.fp8_gemm(a.to(E4), one(M), b.to(E4), one(N), out_dtype=to)
     ref, _ = R.fp8_gemm(a.to(E4), one(M), 1, b.to(E4), one(N), 1)
-    assert float(ref.abs().max()) <= 2048.0 and torch.equal(got.double(), ref)
+    assert float(ref.abs().max()) <= 2048.0 and torch.equal(got, ref.to(to))
 
 
 def test_fp8_gemm_views(scg):
