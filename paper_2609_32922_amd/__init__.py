@@ -53,7 +53,7 @@ def make_desc(A, B, L_max: int, polarity: int, seed: int, L_hint: int = 0,
 
 
 class Workspace:
-    """A reusable device workspace (a torch uint8 tensor, 256-byte aligned)."""
+    """A reusable device workspace (a torch uint8 tensor, 256-byte aligned).  Calls that share one have to be ordered."""
 
     def __init__(self, nbytes: int, device="cuda"):
         import torch
@@ -61,10 +61,18 @@ class Workspace:
         self._buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
         base = self._buf.data_ptr()
         self.ptr = (base + 255) // 256 * 256
+        self._made_on = torch._C._cuda_getCurrentRawStream(self._buf.device.index)
 
     def ensure(self, nbytes: int):
         if nbytes > self.nbytes:
             self.__init__(nbytes, self._buf.device)
+        return self
+
+    def use(self):
+        """Marks it as used by the current stream, so that its memory, when it is given back or grown, waits for that stream too."""
+        import torch
+        if torch._C._cuda_getCurrentRawStream(self._buf.device.index) != self._made_on:
+            self._buf.record_stream(torch.cuda.current_stream(self._buf.device))
         return self
 
 

@@ -3,8 +3,9 @@ norms, gate and residual between two branches of a transformer block with their 
 
 As in the package's other functions torch supplies memory and the stream, and every step runs in the library's kernels.
 Tensors may be views: the last dimension has to be contiguous, the others have any stride that does not lie on itself.
-``stream`` is a torch.cuda.Stream (default: the current one of the tensors' device); tensors made here are marked as used
-by it when it is another.
+``stream`` is a torch.cuda.Stream of the tensors' device (default: the current one).  What is made here comes from that stream's
+memory and is marked as used by the current one too; as with any stream, the inputs have to be ready on it and to live until it has
+read them.
 """
 from __future__ import annotations
 
@@ -59,41 +60,46 @@ class _Plan:
         self.dev, self.index, self.name = dev, dev.index, name
         self.function = getattr(load(), name)
 
-    def stream(self, stream):
-        """(handle, the stream if tensors made here are used on another one than their own)"""
-        import torch
-        if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.index), None
-        return int(stream.cuda_stream), stream if stream != torch.cuda.current_stream(self.dev) else None
-
     def run(self, *args):
+        """The call on the current stream of its device."""
         import torch
         if torch._C._cuda_getDevice() == self.index:
-            rc = self.function(*args)
+            rc = self.function(*args, torch._C._cuda_getCurrentRawStream(self.index))
         else:
             with torch.cuda.device(self.dev):
-                rc = self.function(*args)
+                rc = self.function(*args, torch._C._cuda_getCurrentRawStream(self.index))
         if rc != SC_OK:
             raise ScError(rc, self.name)
 
 
-def _used_on(stream, *tensors):
-    for t in tensors:
+def _on_stream(stream, dev, call):
+    """``call()``, which makes tensors and works on the current stream, on ``stream``.
+
+    Memory that the current stream's tensors have left may still be in use by work that waits there, which ``stream`` knows
+    nothing of.  So what the call makes has to be the other stream's memory, and is marked as used by the current one, on which its
+    user goes on.
+    """
+    import torch
+    if stream.device != dev:
+        raise ValueError("stream must be one of %s" % dev)
+    now = torch.cuda.current_stream(dev)
+    if stream == now:
+        return call()
+    with torch.cuda.stream(stream):
+        got = call()
+    for t in got.values() if isinstance(got, dict) else got if isinstance(got, tuple) else (got,):
         if t is not None:
-            t.record_stream(stream)
+            t.record_stream(now)
+    return got
 
 
-def _workspace(dev, nbytes, given, other):
-    """(address, bytes, what holds it) of a workspace; ``given`` is grown where it is too small."""
+def _workspace(dev, nbytes, given):
+    """(address, bytes, what holds it) of a workspace for the current stream; ``given`` is grown where it is too small."""
     import torch
     if given is not None:
-        given.ensure(nbytes)
-        if other is not None:
-            given._buf.record_stream(other)
+        given.ensure(nbytes).use()
         return given.ptr, given.nbytes, given
     buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
-    if other is not None:
-        buf.record_stream(other)
     return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
 
 
@@ -143,15 +149,14 @@ def fp8_quantize(X, *, dtype=None, block: int = SC_BLOCK_1X128, stream=None):
     transpose's rows, Q [.., K, rows] and scale [.., K, ceil(rows/128)].
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, X.device, lambda: fp8_quantize(X, dtype=dtype, block=block))
     if dtype is None:
         dtype = torch.float8_e4m3fn
     key = ("quantize", X.shape, X.stride(), X.dtype, X.device, dtype, block)
     p = _plans.get(key) or _quantize_plan(key, X, dtype, block)
     Q, scale = torch.empty(p.q_shape, dtype=dtype, device=p.dev), torch.empty(p.s_shape, dtype=p.f32, device=p.dev)
-    handle, other = p.stream(stream)
-    if other is not None:
-        _used_on(other, Q, scale)
-    p.run(*p.head, X.data_ptr(), *p.mid, Q.data_ptr(), *p.q_strides, scale.data_ptr(), *p.s_strides, handle)
+    p.run(*p.head, X.data_ptr(), *p.mid, Q.data_ptr(), *p.q_strides, scale.data_ptr(), *p.s_strides)
     return Q, scale
 
 
@@ -212,16 +217,15 @@ def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=Non
     may lose up to 7 2^-13 of the sum of the products' magnitudes.  Returns out [.., M, N].
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, A.device, lambda: fp8_gemm(A, sA, B, sB, bias=bias, out=out, out_dtype=out_dtype, workspace=workspace))
     key = ("gemm", A.shape, A.stride(), A.dtype, A.device, sA.shape, sA.stride(), sA.dtype, sA.device, B.shape, B.stride(), B.dtype,
            B.device, sB.shape, sB.stride(), sB.dtype, sB.device, out_dtype, _form(bias), _form(out))
     p = _plans.get(key) or _gemm_plan(key, A, sA, B, sB, bias, out, out_dtype)
-    handle, other = p.stream(stream)
     if out is None:
         out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
-        if other is not None:
-            out.record_stream(other)
-    ws = (None, 0, None) if p.nbytes == 0 else _workspace(p.dev, p.nbytes, workspace, other)
-    p.run(p.ref, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), _ptr(bias), out.data_ptr(), ws[0], ws[1], handle)
+    ws = (None, 0, None) if p.nbytes == 0 else _workspace(p.dev, p.nbytes, workspace)
+    p.run(p.ref, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), _ptr(bias), out.data_ptr(), ws[0], ws[1])
     return out
 
 
@@ -295,6 +299,11 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
     there.
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, x.device, lambda: residual_norm(
+            x, y, post=post, pre=pre, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight, pre_bias=pre_bias,
+            res_scale=res_scale, post_offset=post_offset, pre_offset=pre_offset, post_eps=post_eps, pre_eps=pre_eps,
+            out_dtype=out_dtype, want_x=want_x, want_h=want_h, want_rowmax=want_rowmax, inplace=inplace))
     if out_dtype is None:
         out_dtype = x.dtype
     key = ("norm", x.shape, x.stride(), x.dtype, x.device, _form(y), _form(post_weight), _form(post_bias), _form(gate),
@@ -308,11 +317,8 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
     h = torch.empty(p.shape, dtype=out_dtype, device=dev) if want_h else None
     scale = torch.empty(p.s_shape, dtype=p.f32, device=dev) if p.s_shape is not None else None
     rowmax = torch.empty(p.s_shape, dtype=p.f32, device=dev) if want_rowmax else None
-    handle, other = p.stream(stream)
-    if other is not None:
-        _used_on(other, None if inplace else xo, h, scale, rowmax)
     p.run(p.ref, x.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight), _ptr(pre_bias), _ptr(xo),
-          _ptr(h), _ptr(scale), _ptr(rowmax), handle)
+          _ptr(h), _ptr(scale), _ptr(rowmax))
     return xo, h, scale, rowmax
 
 
@@ -359,13 +365,17 @@ def residual_norm_backward(xo, y=None, *, dxo=None, dh=None, post: int = SC_NORM
     the parameter's shape (summed over the rows, and over the batch where it is shared).
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, xo.device, lambda: residual_norm_backward(
+            xo, y, dxo=dxo, dh=dh, post=post, pre=pre, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight,
+            pre_bias=pre_bias, res_scale=res_scale, post_offset=post_offset, pre_offset=pre_offset, post_eps=post_eps,
+            pre_eps=pre_eps, want_x=want_x, want_params=want_params, workspace=workspace))
     key = ("back", xo.shape, xo.stride(), xo.dtype, xo.device, _form(y), _form(dxo), _form(dh), _form(post_weight), _form(post_bias),
            _form(gate), _form(pre_weight), _form(pre_bias), post, pre, res_scale, post_offset, pre_offset, post_eps, pre_eps, want_x,
            want_params)
     p = _plans.get(key) or _backward_plan(key, xo, y, dxo, dh, (post_weight, post_bias, gate, pre_weight, pre_bias), post, pre,
                                           (post_eps, pre_eps, res_scale, post_offset, pre_offset), want_x, want_params)
     dev = p.dev
-    handle, other = p.stream(stream)
     got = {}
     if want_x:
         got["x"] = torch.empty(p.shape, dtype=xo.dtype, device=dev)
@@ -373,13 +383,11 @@ def residual_norm_backward(xo, y=None, *, dxo=None, dh=None, post: int = SC_NORM
         got["y"] = torch.empty(p.shape, dtype=y.dtype, device=dev)
     for shape, names in p.sums.items():
         got.update(zip(names, torch.empty((len(names),) + shape, dtype=torch.float32, device=dev).unbind(0)))
-    if other is not None:
-        _used_on(other, *got.values())
-    ws = (None, 0, None) if p.nbytes == 0 else _workspace(dev, p.nbytes, workspace, other)
+    ws = (None, 0, None) if p.nbytes == 0 else _workspace(dev, p.nbytes, workspace)
     g = got.get
     p.run(p.ref, xo.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight), _ptr(dxo), _ptr(dh),
           _ptr(g("x")), _ptr(g("y")), _ptr(g("post_weight")), _ptr(g("post_bias")), _ptr(g("gate")), _ptr(g("pre_weight")),
-          _ptr(g("pre_bias")), ws[0], ws[1], handle)
+          _ptr(g("pre_bias")), ws[0], ws[1])
     return got
 
 
@@ -462,15 +470,15 @@ def rope(x, pos, freq, axis, *, interleaved: bool = False, inverse: bool = False
     back: the gradient of x from that of the result.  ``out`` may be x itself.  Returns out, like x.
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, x.device, lambda: rope(x, pos, freq, axis, interleaved=interleaved, inverse=inverse, out=out,
+                                                         out_dtype=out_dtype))
     key = ("rope", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved, inverse, out_dtype, _form(out))
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, inverse, out, out_dtype, False)
-    handle, other = p.stream(stream)
     if out is None:
         out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
-        if other is not None:
-            out.record_stream(other)
-    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), out.data_ptr(), None, None, handle)
+    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), out.data_ptr(), None, None)
     return out
 
 
@@ -480,14 +488,13 @@ def rope_quantize(x, pos, freq, axis, *, interleaved: bool = False, want_rowmax:
     Returns (Q int8 [.., heads, tokens, D], scale float32 [.., heads, tokens], rowmax alike or None).
     """
     import torch
+    if stream is not None:
+        return _on_stream(stream, x.device, lambda: rope_quantize(x, pos, freq, axis, interleaved=interleaved, want_rowmax=want_rowmax))
     key = ("rope int8", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved)
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, False, None, None, True)
     Q = torch.empty(p.shape, dtype=torch.int8, device=p.dev)
     scale = torch.empty(p.s_shape, dtype=torch.float32, device=p.dev)
     rowmax = torch.empty(p.s_shape, dtype=torch.float32, device=p.dev) if want_rowmax else None
-    handle, other = p.stream(stream)
-    if other is not None:
-        _used_on(other, Q, scale, rowmax)
-    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), Q.data_ptr(), scale.data_ptr(), _ptr(rowmax), handle)
+    p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), Q.data_ptr(), scale.data_ptr(), _ptr(rowmax))
     return Q, scale, rowmax

@@ -1,5 +1,6 @@
 """The layer operators on the GPU against their definitions in 64 bits (tests/layers_ref.py)."""
 import sys
+import types
 
 import numpy as np
 import pytest
@@ -779,6 +780,100 @@ def test_another_stream_and_two_at_once(scg):
     g = scg.residual_norm_backward(s1["x"], s1["y"], dxo=s1["x"], dh=s1["y"], gate=s1["gate"], stream=streams[0])
     streams[0].synchronize()
     assert torch.equal(out.view_as(want[0]["qk"]), want[0]["qk"]) and torch.isfinite(g["x"]).all()
+
+
+def _long_work():
+    """Some 20 ms of products on the current stream."""
+    a = torch.ones((8192, 8192), dtype=BF16, device="cuda")
+    for _ in range(30):
+        a = torch.mm(a, a.clone())
+    return a
+
+
+def _calls(scg, gen):
+    """A call of each operator that makes tensors, as functions of the stream, with results of more than a megabyte."""
+    x, y = _randn((1100, 1152), gen), _randn((1100, 1152), gen)
+    A, sA = _operand((600, 8192), gen, E4, 1)
+    B, sB = _operand((700, 8192), gen, E4, 128)
+    A2, sA2 = _operand((128, 8192), gen, E4, 1)
+    B2, sB2 = _operand((128, 8192), gen, E4, 128)
+    f, ax = scg.rope_table([64])
+    pos = torch.arange(1100, dtype=torch.int32, device="cuda")[None]
+    heads = x.view(1100, 18, 64)
+    w = _randn((1152,), gen)
+    return [
+        lambda s: scg.fp8_quantize(x, stream=s),
+        lambda s: (scg.fp8_gemm(A, sA, B, sB, out_dtype=F32, stream=s),),
+        lambda s: (scg.fp8_gemm(A2, sA2, B2, sB2, stream=s),),                      # sums of blocks in a workspace
+        lambda s: scg.residual_norm(x, y, out_dtype=torch.int8, want_rowmax=True, stream=s),
+        lambda s: tuple(scg.residual_norm_backward(x, y, dxo=y, dh=x, gate=w, pre_weight=w, stream=s).values()),
+        lambda s: (scg.rope(heads, pos, f, ax, stream=s),),
+        lambda s: scg.rope_quantize(heads, pos, f, ax, want_rowmax=True, stream=s),
+    ]
+
+
+def test_memory_of_a_given_stream(scg):
+    # what a call makes for another stream must not lie where work that waits on the current one still writes
+    _note("memory of a given stream")
+    side = torch.cuda.Stream()
+    for call in _calls(scg, _gen(30)):
+        want = [t for t in call(None) if t is not None]
+        torch.cuda.synchronize()
+        old = [torch.empty_like(t) for t in want] + [torch.empty(4 << 20, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        work = _long_work()
+        for t in old:
+            t.view(torch.uint8).fill_(0x3C)              # (behind that work, when `side` has long been done)
+        left = {t.data_ptr() for t in old}
+        del old, t
+        got = [t for t in call(side) if t is not None]
+        assert not left & {t.data_ptr() for t in got}
+        torch.cuda.synchronize()
+        assert len(got) == len(want) and all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
+        del work
+
+
+def test_stream_of_another_device(scg):
+    _note("stream of another device")
+    there = types.SimpleNamespace(device=torch.device("cuda", torch.cuda.device_count()), cuda_stream=0)
+    for call in _calls(scg, _gen(32)):
+        with pytest.raises(ValueError):
+            call(there)
+
+
+def test_workspace_of_another_stream(scg):
+    # a workspace that was made on one stream and is used and grown on another is not given away before that one is done
+    _note("workspace of another stream")
+    gen = _gen(31)
+    A, sA = _operand((100, 8192), gen, E4, 1)
+    B, sB = _operand((128, 8192), gen, E4, 128)
+    A2, sA2 = _operand((128, 16384), gen, E4, 1)
+    B2, sB2 = _operand((256, 16384), gen, E4, 128)
+    want = scg.fp8_gemm(A, sA, B, sB), scg.fp8_gemm(A2, sA2, B2, sB2)
+    side = torch.cuda.Stream()
+    for given in (False, True):
+        ws = scg.Workspace(2 << 20)
+        for k in range(2):
+            torch.cuda.synchronize()
+            first = ws._buf.data_ptr(), ws._buf.numel()
+            with torch.cuda.stream(side):
+                work = _long_work()
+                one = None if given else scg.fp8_gemm(A, sA, B, sB, workspace=ws)
+            if given:
+                one = scg.fp8_gemm(A, sA, B, sB, workspace=ws, stream=side)
+            assert ws._buf.data_ptr() == first[0]
+            if k == 0:
+                with torch.cuda.stream(side):
+                    two = scg.fp8_gemm(A2, sA2, B2, sB2, workspace=ws)
+                assert ws._buf.data_ptr() != first[0]
+            else:
+                two = want[1]
+                ws = None
+            t = torch.empty(first[1], dtype=torch.uint8, device="cuda")
+            assert t.data_ptr() != first[0]
+            t.fill_(0x3C)
+            torch.cuda.synchronize()
+            assert torch.equal(one, want[0]) and torch.equal(two, want[1])
+            del t, work
 
 
 def test_graph_replays(scg):
