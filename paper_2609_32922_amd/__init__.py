@@ -21,16 +21,14 @@ __all__ = ["gemm", "make_desc", "comparator_sequence", "quantize", "mp_lengths",
            "fp8_quantize", "fp8_gemm", "residual_norm", "residual_norm_backward", "rope", "rope_quantize", "rope_table",
            "SC_BLOCK_1X128", "SC_BLOCK_128X128", "SC_BLOCK_128X1_T", "SC_NORM_NONE", "SC_NORM_RMS", "SC_NORM_LAYER"]
 
-from .layers import (SC_BLOCK_1X128, SC_BLOCK_128X1_T, SC_BLOCK_128X128, SC_NORM_LAYER, SC_NORM_NONE,  # noqa: E402,F401
+from .layers import (_on_stream, SC_BLOCK_1X128, SC_BLOCK_128X1_T, SC_BLOCK_128X128, SC_NORM_LAYER, SC_NORM_NONE,  # noqa: E402,F401
                      SC_NORM_RMS, fp8_gemm, fp8_quantize, residual_norm, residual_norm_backward, rope, rope_quantize, rope_table)
 
 
-def _stream_handle(stream, device_index=None):
-    """The stream's handle, or that of the device's (default: current device's) current stream,
-    read without building a torch.cuda.Stream object (0.2 us of host time instead of 2.7)."""
+def _stream_handle(device_index=None):
+    """The handle of the device's (default: current device's) current stream, read without
+    building a torch.cuda.Stream object (0.2 us of host time instead of 2.7)."""
     import torch
-    if stream is not None:
-        return int(stream.cuda_stream)
     if device_index is None:
         device_index = torch.cuda.current_device()
     return torch._C._cuda_getCurrentRawStream(device_index)
@@ -100,10 +98,14 @@ def gemm(A, sA, B, sB, L, *, L_max: int, polarity: int = SC_BIPOLAR_XNOR, seed: 
     the comparator source (LFSR, or Sobol-8 with conditional generation of B,
     L_max <= 256).  ``out`` (float32) and ``counts`` (int32), when given, must be
     contiguous [batch, M, N] tensors ([M, N] for 2-d A) on A's device.  When ``stream`` is
-    not the current stream, tensors allocated here are marked as used by ``stream``.
-    Returns (out, counts or None).
+    not the current stream, tensors allocated here are that stream's memory and are marked as
+    used by the current one.  Returns (out, counts or None).
     """
     import torch
+    if stream is not None and stream != torch.cuda.current_stream(A.device):
+        return _on_stream(stream, A.device, lambda: gemm(
+            A, sA, B, sB, L, L_max=L_max, polarity=polarity, seed=seed, out=out, counts=counts, want_counts=want_counts,
+            workspace=workspace, check_status=check_status, prof_events=prof_events, L_hint=L_hint, rng=rng))
     squeeze = A.dim() == 2
     d = make_desc(A, B, L_max, polarity, seed, L_hint, rng)
     dev = A.device
@@ -117,32 +119,20 @@ def gemm(A, sA, B, sB, L, *, L_max: int, polarity: int = SC_BIPOLAR_XNOR, seed: 
     if sA.numel() != batch * M or L.numel() != batch * M or sB.numel() != (B.shape[0] if B.dim() == 3 else 1) * N:
         raise ValueError("scale or length vector has the wrong size")
     oshape = (M, N) if squeeze else (batch, M, N)
-    foreign = stream is not None and stream != torch.cuda.current_stream(dev)
-    made = []
     if out is None:
         out = torch.empty(oshape, dtype=torch.float32, device=dev)
-        made.append(out)
     else:
         _check_output(out, "out", torch.float32, oshape, dev)
     if counts is None and want_counts:
         counts = torch.empty(oshape, dtype=torch.int32, device=dev)
-        made.append(counts)
     elif counts is not None:
         _check_output(counts, "counts", torch.int32, oshape, dev)
     nbytes = sc_gemm_workspace_size(d)
-    if workspace is None:
-        ws = Workspace(nbytes, dev)
-        made.append(ws._buf)
-    else:
-        ws = workspace.ensure(nbytes)
-    if foreign:
-        # the caching allocator must not hand these blocks out again before `stream` is done
-        for t in made:
-            t.record_stream(stream)
+    ws = Workspace(nbytes, dev) if workspace is None else workspace.ensure(nbytes).use()
     if prof_events is not None:
         d.prof_event_begin = prof_events[0]
         d.prof_event_end = prof_events[1]
-    sh = _stream_handle(stream, dev.index)
+    sh = _stream_handle(dev.index)
     rc = sc_gemm(d, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), L.data_ptr(),
                  out.data_ptr(), counts.data_ptr() if counts is not None else 0, ws.ptr, ws.nbytes, sh)
     if rc != SC_OK:
@@ -157,8 +147,10 @@ def gemm(A, sA, B, sB, L, *, L_max: int, polarity: int = SC_BIPOLAR_XNOR, seed: 
 def comparator_sequence(seed: int, op: int, n: int, stream=None, rng: int = SC_RNG_LFSR32):
     """Device comparator sequence r_0..r_{n-1} (uint8 tensor) of operand ``op``."""
     import torch
+    if stream is not None:
+        return _on_stream(stream, stream.device, lambda: comparator_sequence(seed, op, n, rng=rng))
     out = torch.empty(n, dtype=torch.uint8, device="cuda")
-    rc = sc_comparator_sequence(seed, op, rng, n, out.data_ptr(), _stream_handle(stream))
+    rc = sc_comparator_sequence(seed, op, rng, n, out.data_ptr(), _stream_handle())
     if rc != SC_OK:
         raise ScError(rc, "sc_comparator_sequence")
     return out
@@ -172,6 +164,8 @@ def quantize(X, per_tensor: bool = False, want_rowmax: bool = False, stream=None
     import torch
     if not X.is_cuda or not X.is_contiguous() or X.dtype != torch.float32:
         raise ValueError("X must be a contiguous float32 device tensor")
+    if stream is not None:
+        return _on_stream(stream, X.device, lambda: quantize(X, per_tensor, want_rowmax))
     shape, dev = X.shape, X.device
     batch, rows, K = shape if X.dim() != 2 else (1, *shape)
     # the outputs are made in the caller's rank: a view of each costs the host 1 us, and the
@@ -181,7 +175,7 @@ def quantize(X, per_tensor: bool = False, want_rowmax: bool = False, stream=None
     rowmax = torch.empty(shape[:-1], dtype=torch.float32, device=dev) if want_rowmax else None
     rc = sc_quantize(batch, rows, K, X.data_ptr(), K, rows * K, int(per_tensor), Q.data_ptr(), K,
                      rows * K, scale.data_ptr(), rowmax.data_ptr() if rowmax is not None else 0,
-                     rows, _stream_handle(stream))
+                     rows, _stream_handle())
     if rc != SC_OK:
         raise ScError(rc, "sc_quantize")
     return Q, scale, rowmax
@@ -193,10 +187,12 @@ def mp_lengths(metric, tau, ladder, stream=None):
     import torch
     if not metric.is_cuda or not metric.is_contiguous() or metric.dtype != torch.float32:
         raise ValueError("metric must be a contiguous float32 device tensor")
+    if stream is not None:
+        return _on_stream(stream, metric.device, lambda: mp_lengths(metric, tau, ladder))
     batch, M = metric.shape if metric.dim() != 1 else (1, *metric.shape)
     L = torch.empty(metric.shape, dtype=torch.int32, device=metric.device)
     rc = sc_mp_lengths(batch, M, metric.data_ptr(), M, list(tau), list(ladder), L.data_ptr(), M,
-                       _stream_handle(stream))
+                       _stream_handle())
     if rc != SC_OK:
         raise ScError(rc, "sc_mp_lengths")
     return L

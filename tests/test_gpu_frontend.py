@@ -260,3 +260,47 @@ def test_binding_ranks_and_current_stream(dev, oracle_mod, shape):
     A = x.cpu().numpy().reshape(-1, shape[-1])
     absmax = np.abs(A).max(axis=1)
     assert np.array_equal(want[2].cpu().numpy().reshape(-1), absmax)
+
+
+def test_binding_memory_of_a_given_stream(dev):
+    """What a call makes for a given stream does not lie where work that waits on the current
+    one still writes; a workspace made on the current one stays until that stream is done."""
+    import torch
+    import paper_2609_32922_amd as scg
+    from test_gpu_layers import _long_work
+    _note("binding: memory of a given stream")
+    g = torch.Generator(device="cpu").manual_seed(12)
+    x = torch.randn((1200, 1100), generator=g).to(dev)
+    q, s, m = scg.quantize(x, want_rowmax=True)
+    metric = torch.rand(600000, generator=g).to(dev)
+    L = torch.full((1200,), 32, dtype=torch.int32, device=dev)
+    side = torch.cuda.Stream()
+    calls = [lambda st: scg.quantize(x, want_rowmax=True, stream=st),
+             lambda st: (scg.mp_lengths(metric, [0.5], [64, 32], stream=st),),
+             lambda st: (scg.comparator_sequence(3, 0, 4096, stream=st),),
+             lambda st: scg.gemm(q, s, q, s, L, L_max=32, seed=3, want_counts=True, stream=st)]
+    for call in calls:
+        want = call(None)
+        torch.cuda.synchronize()
+        old = [torch.empty_like(t) for t in want]
+        work = _long_work()
+        for t in old:
+            t.view(torch.uint8).fill_(0x3C)
+        left = {t.data_ptr() for t in old}
+        del old, t
+        got = call(side)
+        assert not left & {t.data_ptr() for t in got}
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del work
+    ws = scg.Workspace(scg.sc_gemm_workspace_size(scg.make_desc(q, q, 32, 0, 3)), dev)
+    first, size = ws._buf.data_ptr(), ws._buf.numel()
+    with torch.cuda.stream(side):
+        work = _long_work()
+        got = scg.gemm(q, s, q, s, L, L_max=32, seed=3, workspace=ws)[0]
+    ws = None
+    t = torch.empty(size, dtype=torch.uint8, device=dev)
+    assert t.data_ptr() != first
+    t.fill_(0x3C)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want[0])
