@@ -57,6 +57,8 @@ class Workspace:
         import torch
         self.nbytes = int(nbytes)
         self._buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device)
+        if not self._buf.is_cuda:
+            raise ValueError("a workspace lies on a GPU, not on %s" % device)
         base = self._buf.data_ptr()
         self.ptr = (base + 255) // 256 * 256
         self._made_on = torch._C._cuda_getCurrentRawStream(self._buf.device.index)
@@ -66,9 +68,12 @@ class Workspace:
             self.__init__(nbytes, self._buf.device)
         return self
 
-    def use(self):
-        """Marks it as used by the current stream, so that its memory, when it is given back or grown, waits for that stream too."""
+    def use(self, device):
+        """Marks it as used by the current stream of ``device``, which has to be its own, so that its memory, when it is given
+        back or grown, waits for that stream too."""
         import torch
+        if self._buf.device != device:
+            raise ValueError("workspace must be on %s, not %s" % (device, self._buf.device))
         if torch._C._cuda_getCurrentRawStream(self._buf.device.index) != self._made_on:
             self._buf.record_stream(torch.cuda.current_stream(self._buf.device))
         return self
@@ -128,7 +133,7 @@ def gemm(A, sA, B, sB, L, *, L_max: int, polarity: int = SC_BIPOLAR_XNOR, seed: 
     elif counts is not None:
         _check_output(counts, "counts", torch.int32, oshape, dev)
     nbytes = sc_gemm_workspace_size(d)
-    ws = Workspace(nbytes, dev) if workspace is None else workspace.ensure(nbytes).use()
+    ws = Workspace(nbytes, dev) if workspace is None else workspace.ensure(nbytes).use(dev)
     if prof_events is not None:
         d.prof_event_begin = prof_events[0]
         d.prof_event_end = prof_events[1]

@@ -97,7 +97,7 @@ def _workspace(dev, nbytes, given):
     """(address, bytes, what holds it) of a workspace for the current stream; ``given`` is grown where it is too small."""
     import torch
     if given is not None:
-        given.ensure(nbytes).use()
+        given.ensure(nbytes).use(dev)
         return given.ptr, given.nbytes, given
     buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=dev)
     return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf

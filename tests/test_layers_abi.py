@@ -218,3 +218,15 @@ def test_rope_refuses_pointers(lib):
     for empty in (dict(batch=0), dict(tokens=0), dict(heads=0)):
         assert lib.sc_rope(_rope(lib, **empty), *[0] * 7, 0) == lib.SC_OK
     assert lib.load().sc_rope(None, *[None] * 8) == lib.SC_ERR_NULL
+
+
+def test_workspace_of_another_device(lib):
+    import torch
+    import paper_2609_32922_amd as scg
+    with pytest.raises(ValueError):
+        scg.Workspace(64, device="cpu")
+    # (one that lies there already, as a call finds it)
+    ws = scg.Workspace.__new__(scg.Workspace)
+    ws.nbytes, ws._buf, ws._made_on = 64, torch.empty(320, dtype=torch.uint8), 0
+    with pytest.raises(ValueError):
+        ws.ensure(0).use(torch.device("cuda", 0))
