@@ -348,10 +348,10 @@ __device__ __forceinline__ Buffer scalar(Buffer s) {      // (it is the same in 
                   (uint32_t)__builtin_amdgcn_readfirstlane((int)s[2]), 0x00020000u};
 }
 __device__ __forceinline__ void copy16(Buffer s, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory", "m0");
 }
 __device__ __forceinline__ void copy4(Buffer s, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(scalar(s)) : "memory", "m0");
 }
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {

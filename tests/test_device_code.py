@@ -102,3 +102,15 @@ def test_no_store_data_overwritten(tmp_path):
         found += overwritten_stores(code)
     assert stores > 100          # (the reader still finds the stores)
     assert not found, "\n".join(found)
+
+
+def test_inline_code_names_m0_where_it_writes_it():
+    # the compiler keeps values of its own in m0, and knows only from the list that one is gone
+    import paper_2609_32922_amd.build as build
+    blocks = []
+    for f in sorted(os.listdir(build.CSRC)):
+        with open(os.path.join(build.CSRC, f)) as src:
+            blocks += [b for b in re.findall(r"asm volatile\((.*?)\);", src.read(), re.S) if re.search(r"s_mov_b32 m0", b)]
+    assert blocks                # (the reader still finds them)
+    for b in blocks:
+        assert '"m0"' in b.rsplit(":", 1)[1], b
