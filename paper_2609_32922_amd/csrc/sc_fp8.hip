@@ -977,8 +977,7 @@ static int check_gemm(const sc_fp8_gemm_desc *d) {
     if (d->lda < d->K || d->ldb < d->K || d->ldo < d->N || d->ldsA < kb || d->ldsB < kb) return SC_ERR_STRIDE;
     if (d->strideA < 0 || d->strideB < 0 || d->strideO < 0 || d->strideSA < 0 || d->strideSB < 0 || d->strideBias < 0)
         return SC_ERR_STRIDE;
-    // (batch entries of the output must not lie on top of each other)
-    if (d->batch > 1 && d->M > 0 && d->N > 0 && d->strideO < (int64_t)(d->M - 1) * d->ldo + d->N) return SC_ERR_STRIDE;
+    if (!rows_apart(d->batch, d->strideO, d->M, d->ldo, d->N)) return SC_ERR_STRIDE;
     const int64_t tiles = (((int64_t)d->M + 63) / 64) * (((int64_t)d->N + 31) / 32);
     if (tiles > INT32_MAX) return SC_ERR_SHAPE;
     return SC_OK;
@@ -1001,7 +1000,7 @@ int sc_fp8_quantize(int32_t batch, int32_t rows, int32_t K, int32_t typeX, const
     const int64_t qrows = turned ? K : rows, qcols = turned ? rows : K;
     const int64_t srows = block == SC_BLOCK_128X128 ? RB : qrows, scols = turned ? RB : KB;
     if (ldx < K || ldq < qcols || lds < scols || strideX < 0 || strideQ < 0 || strideS < 0) return SC_ERR_STRIDE;
-    if (batch > 1 && rows > 0 && K > 0 && (strideQ < (qrows - 1) * ldq + qcols || strideS < (srows - 1) * lds + scols))
+    if (rows > 0 && K > 0 && (!rows_apart(batch, strideQ, qrows, ldq, qcols) || !rows_apart(batch, strideS, srows, lds, scols)))
         return SC_ERR_STRIDE;
     if ((int64_t)rows * KB > INT32_MAX || (int64_t)RB * ((K + 63) / 64) > INT32_MAX) return SC_ERR_SHAPE;
     if (batch == 0 || rows == 0 || K == 0) return SC_OK;

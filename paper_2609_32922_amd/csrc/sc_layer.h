@@ -209,6 +209,32 @@ __device__ __forceinline__ void store_bytes4(void *p, int64_t at, uint32_t w, in
     }
 }
 
+// Whether no two of the n0 x n1 x n2 runs of `unit` elements at strides s0, s1, s2 coincide, as a sufficient test: taken by
+// growing stride, each stride passes what the smaller ones span
+inline bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t unit) {
+    int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (s[j] < s[i]) {
+                const int64_t tn = n[i], ts = s[i];
+                n[i] = n[j];
+                s[i] = s[j];
+                n[j] = tn;
+                s[j] = ts;
+            }
+    __int128 span = unit;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] <= 1) continue;
+        if (s[i] < span) return false;
+        span += (__int128)(n[i] - 1) * s[i];
+    }
+    return true;
+}
+// the same of rows of `unit` elements in batch entries; nothing coincides where nothing is written
+inline bool rows_apart(int64_t batch, int64_t stride, int64_t rows, int64_t ld, int64_t unit) {
+    return rows == 0 || unit == 0 || apart(batch, stride, rows, ld, 1, 0, unit);
+}
+
 // A grid of `blocks` blocks for each of `batch` entries: a launch holds fewer than 2^32 threads along a
 // dimension, so blocks go on in rows of 2^20; entries past the third dimension's are taken in turn.
 inline dim3 grid_of(uint32_t blocks, int batch) {

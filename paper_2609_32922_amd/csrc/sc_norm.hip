@@ -635,9 +635,9 @@ static int check_norm(const sc_norm_desc *d) {
     if (is_fp8_type(d->typeH) && d->lds < (D + FP8_BLOCK - 1) / FP8_BLOCK) return SC_ERR_STRIDE;
     return SC_OK;
 }
-// entries of something written must not lie on top of each other
+// rows of something written must not lie on top of each other
 static bool entries_apart(const sc_norm_desc &d, int64_t ld, int64_t stride) {
-    return d.batch <= 1 || d.rows == 0 || d.D == 0 || stride >= (int64_t)(d.rows - 1) * ld + d.D;
+    return rows_apart(d.batch, stride, d.rows, ld, d.D);
 }
 static bool quads(const void *p, int type, int64_t ld, int64_t stride) {
     const int64_t b = type_bytes(type);
@@ -708,7 +708,7 @@ int sc_residual_norm(const sc_norm_desc *desc, const void *x, const void *y, con
         return SC_ERR_STRIDE;
     const bool quantised = !is_float_type(d.typeH);
     const int64_t srow = is_fp8_type(d.typeH) ? d.lds : 1, slen = is_fp8_type(d.typeH) ? (d.D + FP8_BLOCK - 1) / FP8_BLOCK : 1;
-    if (h != nullptr && quantised && d.batch > 1 && d.rows > 0 && d.strideS < (int64_t)(d.rows - 1) * srow + slen) return SC_ERR_STRIDE;
+    if (h != nullptr && quantised && !rows_apart(d.batch, d.strideS, d.rows, srow, slen)) return SC_ERR_STRIDE;
     if (d.batch == 0 || d.rows == 0 || (d.D == 0 && d.typeH != SC_INT8)) return SC_OK;
     if (xo == nullptr && h == nullptr) return SC_OK;
     if (d.D > 0 && x == nullptr) return SC_ERR_NULL;

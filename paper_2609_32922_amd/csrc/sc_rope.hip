@@ -174,28 +174,6 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, uint32_t blocks, int s
     }
 }
 
-// Whether no two of the n_i elements at strides s_i coincide, as a sufficient test: taken by growing stride, each
-// stride passes what the smaller ones span
-static bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t unit) {
-    int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
-    for (int i = 0; i < 3; ++i)
-        for (int j = i + 1; j < 3; ++j)
-            if (s[j] < s[i]) {
-                const int64_t tn = n[i], ts = s[i];
-                n[i] = n[j];
-                s[i] = s[j];
-                n[j] = tn;
-                s[j] = ts;
-            }
-    int64_t span = unit;
-    for (int i = 0; i < 3; ++i) {
-        if (n[i] <= 1) continue;
-        if (s[i] < span) return false;
-        span += (n[i] - 1) * s[i];
-    }
-    return true;
-}
-
 template <bool VEC, int R, bool STREAM, bool INT8>
 static void launch_rope(const RopeArgs &a, bool near, dim3 grid, uint32_t blocks, int shift, hipStream_t st) {
     if (near) hipLaunchKernelGGL((k_rope<VEC, true, R, STREAM, INT8>), grid, dim3(256), 0, st, a, blocks, shift);

@@ -256,6 +256,21 @@ def test_fp8_gemm_of_columns_of_padded_rows(scg, M, N, K, ld, to):
     _within(got, ref, R.gemm_tolerance(mag, K, to, ref), "product")
 
 
+@pytest.mark.parametrize("to", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", [(5, 64, 128), (150, 72, 300), (70, 99, 4000), (700, 640, 256), (701, 643, 256)])
+def test_fp8_gemm_into_rows_of_entries_in_turn(scg, M, N, K, to):
+    # the result of [heads, rows, n] in memory as [rows, heads, n], with columns beside it that stay as they were
+    _note("fp8_gemm into [rows, heads, n] %d x %d x %d %s" % (M, N, K, to))
+    gen, H = _gen(M + N), 7
+    A, sA = _operand((H, M, K), gen, E4, 1)
+    B, sB = _operand((H, N, K), gen, E4, 1)
+    want = scg.fp8_gemm(A, sA, B, sB, out_dtype=to)
+    big = torch.full((M, H, N + 8), -3.0, dtype=to, device="cuda")
+    out = big[:, :, :N].transpose(0, 1)
+    got = scg.fp8_gemm(A, sA, B, sB, out=out)
+    assert got is out and torch.equal(out, want) and bool((big[:, :, N:] == -3.0).all())
+
+
 def test_fp8_gemm_special_values(scg):
     # NaN and infinities reach their own rows and columns, and nothing else; what lies behind K never counts
     _note("fp8_gemm special values")
@@ -434,6 +449,19 @@ def test_residual_norm_forms(scg):
         z = torch.zeros((rows, 0 if rows else 8), device="cuda")
         xo, h, _, _ = scg.residual_norm(z, z)
         assert xo.shape == z.shape and h.shape == z.shape
+
+
+def test_residual_norm_over_rows_of_entries_in_turn(scg):
+    # x as a view [batch, tokens, D] of a sequence-first buffer, written in place
+    _note("residual_norm in place of a sequence-first buffer")
+    gen = _gen(17)
+    for T, B, D in ((33, 3, 1152), (40, 2, 777), (5, 4, 64)):
+        buf = _randn((T, B, D + 8), gen, BF16)
+        x, y, g = buf[:, :, :D].transpose(0, 1), _randn((B, T, D), gen, BF16), _randn((B, D), gen, BF16)
+        keep, beside = x.clone(), buf[:, :, D:].clone()
+        want = scg.residual_norm(keep, y, gate=g)
+        xo, h, _, _ = scg.residual_norm(x, y, gate=g, inplace=True)
+        assert xo is x and torch.equal(x, want[0]) and torch.equal(h, want[1]) and torch.equal(buf[:, :, D:], beside)
 
 
 def test_residual_norm_special_values(scg):

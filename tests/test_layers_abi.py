@@ -230,3 +230,18 @@ def test_workspace_of_another_device(lib):
     ws.nbytes, ws._buf, ws._made_on = 64, torch.empty(320, dtype=torch.uint8), 0
     with pytest.raises(ValueError):
         ws.ensure(0).use(torch.device("cuda", 0))
+
+
+@pytest.mark.parametrize("stride,ld,apart", [(48, 96, True), (47, 96, False), (48, 95, False), (64 * 48, 48, True), (64 * 48 - 1, 48, False),
+                                             (1 << 40, 48, True), (48, 1 << 40, True), (0, 96, False)])
+def test_rows_of_entries_may_alternate(lib, stride, ld, apart):
+    # the result [2, 64, 48] of strides (stride, ld)
+    so, n, d = lib.load(), ctypes.c_size_t(0), _gemm(lib, ldo=ld, strideO=stride)
+    assert so.sc_fp8_gemm_workspace_size(ctypes.byref(d), ctypes.byref(n)) == (lib.SC_OK if apart else lib.SC_ERR_STRIDE)
+    if not apart:
+        norm = dict(rows=64, D=48, ldx=ld, strideX=stride, ldy=ld, ldxo=ld, strideXO=stride, ldh=ld, strideH=stride, lddxo=ld, lddy=ld,
+                    strideDY=stride)
+        assert lib.sc_residual_norm(_norm(lib, **norm), *[FAKE] * 10, 0, 0) == lib.SC_ERR_STRIDE
+        assert lib.sc_residual_norm_backward(_norm(lib, **norm), *[FAKE] * 16, 1 << 40, 0) == lib.SC_ERR_STRIDE
+        quant = dict(QUANT, rows=64, K=48, ldx=48, ldq=ld, strideQ=stride)
+        assert lib.sc_fp8_quantize(*quant.values(), 0) == lib.SC_ERR_STRIDE
