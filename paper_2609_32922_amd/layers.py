@@ -6,6 +6,9 @@ Tensors may be views: the last dimension has to be contiguous, the others have a
 ``stream`` is a torch.cuda.Stream of the tensors' device (default: the current one).  What is made here comes from that stream's
 memory and is marked as used by the current one too; as with any stream, the inputs have to be ready on it and to live until it has
 read them.
+
+Nothing here is recorded by autograd.  Where gradients are recorded (torch.is_grad_enabled) and a tensor of a forward call requires
+one, the call is refused: call it under torch.no_grad(), and ``residual_norm_backward`` or ``rope(inverse=True)`` for the gradients.
 """
 from __future__ import annotations
 
@@ -103,6 +106,20 @@ def _workspace(dev, nbytes, given):
     return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
 
 
+def _unrecorded(*tensors):
+    """Refuses tensors whose gradient would be lost without a word."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("a tensor requires a gradient, and autograd does not record this call: call it under torch.no_grad()")
+
+
+def _written(t):
+    """Tells autograd that a caller's tensor has changed, as torch's own writes do."""
+    import torch
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _on(t, name, dev):
     if not t.is_cuda or t.device != dev:
         raise ValueError("%s must be on %s" % (name, dev))
@@ -151,6 +168,8 @@ def fp8_quantize(X, *, dtype=None, block: int = SC_BLOCK_1X128, stream=None):
     import torch
     if stream is not None:
         return _on_stream(stream, X.device, lambda: fp8_quantize(X, dtype=dtype, block=block))
+    if torch.is_grad_enabled():
+        _unrecorded(X)
     if dtype is None:
         dtype = torch.float8_e4m3fn
     key = ("quantize", X.shape, X.stride(), X.dtype, X.device, dtype, block)
@@ -219,13 +238,18 @@ def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=Non
     import torch
     if stream is not None:
         return _on_stream(stream, A.device, lambda: fp8_gemm(A, sA, B, sB, bias=bias, out=out, out_dtype=out_dtype, workspace=workspace))
+    if torch.is_grad_enabled():
+        _unrecorded(A, sA, B, sB, bias, out)
     key = ("gemm", A.shape, A.stride(), A.dtype, A.device, sA.shape, sA.stride(), sA.dtype, sA.device, B.shape, B.stride(), B.dtype,
            B.device, sB.shape, sB.stride(), sB.dtype, sB.device, out_dtype, _form(bias), _form(out))
     p = _plans.get(key) or _gemm_plan(key, A, sA, B, sB, bias, out, out_dtype)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
     ws = (None, 0, None) if p.nbytes == 0 else _workspace(p.dev, p.nbytes, workspace)
     p.run(p.ref, A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), _ptr(bias), out.data_ptr(), ws[0], ws[1])
+    if given:
+        _written(out)
     return out
 
 
@@ -304,6 +328,8 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
             x, y, post=post, pre=pre, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight, pre_bias=pre_bias,
             res_scale=res_scale, post_offset=post_offset, pre_offset=pre_offset, post_eps=post_eps, pre_eps=pre_eps,
             out_dtype=out_dtype, want_x=want_x, want_h=want_h, want_rowmax=want_rowmax, inplace=inplace))
+    if torch.is_grad_enabled():
+        _unrecorded(x, y, post_weight, post_bias, gate, pre_weight, pre_bias)
     if out_dtype is None:
         out_dtype = x.dtype
     key = ("norm", x.shape, x.stride(), x.dtype, x.device, _form(y), _form(post_weight), _form(post_bias), _form(gate),
@@ -319,6 +345,8 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
     rowmax = torch.empty(p.s_shape, dtype=p.f32, device=dev) if want_rowmax else None
     p.run(p.ref, x.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight), _ptr(pre_bias), _ptr(xo),
           _ptr(h), _ptr(scale), _ptr(rowmax))
+    if inplace:
+        _written(x)
     return xo, h, scale, rowmax
 
 
@@ -473,12 +501,17 @@ def rope(x, pos, freq, axis, *, interleaved: bool = False, inverse: bool = False
     if stream is not None:
         return _on_stream(stream, x.device, lambda: rope(x, pos, freq, axis, interleaved=interleaved, inverse=inverse, out=out,
                                                          out_dtype=out_dtype))
+    if torch.is_grad_enabled():
+        _unrecorded(x, freq, out)
     key = ("rope", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved, inverse, out_dtype, _form(out))
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, inverse, out, out_dtype, False)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(p.shape, dtype=p.dtype, device=p.dev)
     p.run(p.ref, x.data_ptr(), pos.data_ptr(), freq.data_ptr(), axis.data_ptr(), out.data_ptr(), None, None)
+    if given:
+        _written(out)
     return out
 
 
@@ -490,6 +523,8 @@ def rope_quantize(x, pos, freq, axis, *, interleaved: bool = False, want_rowmax:
     import torch
     if stream is not None:
         return _on_stream(stream, x.device, lambda: rope_quantize(x, pos, freq, axis, interleaved=interleaved, want_rowmax=want_rowmax))
+    if torch.is_grad_enabled():
+        _unrecorded(x, freq)
     key = ("rope int8", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved)
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, False, None, None, True)

@@ -904,6 +904,30 @@ def test_workspace_of_another_stream(scg):
             del t, work
 
 
+def test_writes_over_saved_tensors_are_seen(scg):
+    # a tensor that autograd has saved and that a call writes over: the backward pass raises, and uses no changed value
+    _note("writes over saved tensors")
+    gen = _gen(33)
+    A, sA = _operand((64, 128), gen, E4, 1)
+    freq, axis = scg.rope_table([64])
+    pos = torch.arange(64, dtype=torch.int32, device="cuda")[None]
+    calls = [lambda t: scg.residual_norm(t, t.clone(), inplace=True), lambda t: scg.fp8_gemm(A, sA, A, sA, out=t),
+             lambda t: scg.rope(t.view(64, 1, 64), pos, freq, axis, out=t.view(64, 1, 64))]
+    for call in calls:
+        w, t = torch.ones(64, 64, device="cuda", requires_grad=True), _randn((64, 64), gen)
+        loss = (w * t).sum()
+        call(t)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        with torch.inference_mode():
+            call(torch.zeros(64, 64, device="cuda"))
+    # parameters without recording, and their gradients asked for by name
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    with torch.no_grad():
+        xo, h, _, _ = scg.residual_norm(t, pre_weight=w)
+    assert not h.requires_grad and set(scg.residual_norm_backward(xo, dh=h, pre_weight=w)) == {"x", "pre_weight"}
+
+
 def test_graph_replays(scg):
     _note("graphs")
     s = _block_state(scg, _gen(12))

@@ -245,3 +245,24 @@ def test_rows_of_entries_may_alternate(lib, stride, ld, apart):
         assert lib.sc_residual_norm_backward(_norm(lib, **norm), *[FAKE] * 16, 1 << 40, 0) == lib.SC_ERR_STRIDE
         quant = dict(QUANT, rows=64, K=48, ldx=48, ldq=ld, strideQ=stride)
         assert lib.sc_fp8_quantize(*quant.values(), 0) == lib.SC_ERR_STRIDE
+
+
+def test_tensors_that_require_gradients_are_refused(lib):
+    # (before anything else is looked at; without recording the call goes on, here to its refusal of tensors on the CPU)
+    import torch
+    import paper_2609_32922_amd as scg
+    z = torch.zeros
+    E4 = torch.float8_e4m3fn
+    g = lambda *shape: z(*shape, requires_grad=True)  # noqa: E731
+    pos, freq, axis = z(1, 4, dtype=torch.int32), z(32, dtype=torch.float64), z(32, dtype=torch.int32)
+    a, s = z(4, 64).to(E4), z(4, 1)
+    calls = [lambda: scg.fp8_quantize(g(4, 64)), lambda: scg.fp8_gemm(a, s, a, s, bias=g(4)), lambda: scg.fp8_gemm(a, g(4, 1), a, s),
+             lambda: scg.fp8_gemm(a, s, a, s, out=g(4, 4)), lambda: scg.residual_norm(g(4, 64)), lambda: scg.residual_norm(z(4, 64), g(4, 64)),
+             lambda: scg.residual_norm(z(4, 64), pre_weight=g(64)), lambda: scg.residual_norm(z(4, 64), z(4, 64), gate=g(64)),
+             lambda: scg.rope(g(4, 2, 64), pos, freq, axis), lambda: scg.rope(z(4, 2, 64), pos, freq, axis, out=g(4, 2, 64)),
+             lambda: scg.rope_quantize(g(4, 2, 64), pos, freq, axis)]
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call()
