@@ -1053,6 +1053,8 @@ int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, co
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     size_t la, lb;
     lay_sizes(g, &la, &lb);
+    // (an operand that starts off 16 bytes, which its strides do not say, keeps both from the tiles that the other is laid out for)
+    if ((la == 0 && !aligned_to(A, 16)) || (lb == 0 && !aligned_to(B, 16))) la = lb = 0;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     if (la > 0 && lay(&g.A, &g.lda, &g.strideA, g.M, g, ws, st) != hipSuccess) return SC_ERR_HIP;
     if (lb > 0 && lay(&g.B, &g.ldb, &g.strideB, g.N, g, ws + la, st) != hipSuccess) return SC_ERR_HIP;

@@ -271,6 +271,26 @@ def test_fp8_gemm_into_rows_of_entries_in_turn(scg, M, N, K, to):
     assert got is out and torch.equal(out, want) and bool((big[:, :, N:] == -3.0).all())
 
 
+def test_fp8_gemm_lays_nothing_out_for_nothing(scg):
+    # one operand off 16 bytes, the other with rows that would be laid out for the tiles which the first one keeps both from
+    _note("fp8_gemm off 16 bytes beside odd rows")
+    gen = _gen(18)
+    M, N, K = 1500, 1411, 200
+    odd, row = torch.zeros(M * 256 + 1, dtype=torch.uint8, device="cuda"), torch.zeros((N, 203), dtype=torch.uint8, device="cuda")
+    (a, sA), (b, sB) = _operand((M, K), gen, E4, 1), _operand((N, K), gen, E4, 128)
+    A, B = odd[1:].view(M, 256)[:, :K], row[:, :K]
+    A.copy_(a.view(torch.uint8))
+    B.copy_(b.view(torch.uint8))
+    ws = scg.Workspace(1 << 20)
+    ws._buf.fill_(0x3C)
+    for x, sx, y, sy in ((A, sA, B, sB), (B, sB, A, sA)):
+        got = scg.fp8_gemm(x.view(E4), sx, y.view(E4), sy, out_dtype=F32, workspace=ws)
+        px, py = ((1, 128) if x is A else (128, 1))
+        ref, mag = R.fp8_gemm(x.view(E4), sx, px, y.view(E4), sy, py)
+        _within(got, ref, R.gemm_tolerance(mag, K, F32, ref), "product")
+    assert bool((ws._buf == 0x3C).all())
+
+
 def test_fp8_gemm_special_values(scg):
     # NaN and infinities reach their own rows and columns, and nothing else; what lies behind K never counts
     _note("fp8_gemm special values")
