@@ -471,6 +471,30 @@ def test_residual_norm_forms(scg):
         assert xo.shape == z.shape and h.shape == z.shape
 
 
+@pytest.mark.parametrize("D", [64, 300, 777, 2500])
+def test_int8_rows_of_special_values(scg, D):
+    # NaN, infinities, zeros, the least and the largest floats: what the quantisers make of them
+    _note("int8 rows of special values D=%d" % D)
+    gen = _gen(D)
+    x = _randn((12, D), gen)
+    x[1, 3], x[2, 4], x[3, 5], x[4], x[5], x[6] = float("nan"), float("inf"), -float("inf"), 0.0, 1e-45, 3e38
+    x[7, :2], x[8], x[9] = 1e-38, float("nan"), 2.0 ** -140
+    _, q, s, m = scg.residual_norm(x, pre=0, out_dtype=torch.int8, want_rowmax=True)
+    for a, b in zip((q, s, m), scg.quantize(x, want_rowmax=True)):
+        assert torch.equal(a, b)
+    for t in (E4, E5):
+        _, q, s, _ = scg.residual_norm(x, pre=0, out_dtype=t)
+        qr, sr = scg.fp8_quantize(x, dtype=t)
+        assert torch.equal(s, sr)
+        _same_bytes(q, qr)
+    if D <= 256:
+        f, ax = scg.rope_table([D])
+        heads, pos = x.view(12, 1, D), torch.zeros(1, 12, dtype=torch.int32, device="cuda")
+        turned = scg.rope(heads, pos, f, ax).transpose(0, 1).contiguous()
+        for a, b in zip(scg.rope_quantize(heads, pos, f, ax, want_rowmax=True), scg.quantize(turned, want_rowmax=True)):
+            assert torch.equal(a, b)
+
+
 def test_residual_norm_over_rows_of_entries_in_turn(scg):
     # x as a view [batch, tokens, D] of a sequence-first buffer, written in place
     _note("residual_norm in place of a sequence-first buffer")
@@ -755,6 +779,36 @@ def test_rope_there_and_back_and_views(scg):
     _within(scg.rope(x, pos, freq, bad)[None], ref, 8 * R.U * mag + 1e-30, "axes outside")
 
 
+def test_more_entries_than_a_grid_holds(scg):
+    _note("40000 entries")
+    gen, n = _gen(35), 40000
+    x = _randn((n, 2, 136), gen)
+    for block, per in ((0, 1), (1, 128), (2, 1)):
+        Q, s = scg.fp8_quantize(x, block=block)
+        Qr, sr = R.fp8_quantize32(x.transpose(1, 2).contiguous() if block == 2 else x, E4, per)
+        assert torch.equal(s, sr)
+        _same_bytes(Q, Qr)
+    for M in (2, 17):
+        A, sA = _operand((n, M, 130), gen, E4, 1)
+        for lead in ((n,), ()):
+            B, sB = _operand((*lead, 5, 130), gen, E4, 1)
+            got = scg.fp8_gemm(A, sA, B, sB)
+            ref, mag = R.fp8_gemm(A, sA, 1, B, sB, 1)
+            _within(got, ref, R.gemm_tolerance(mag, 130, BF16, ref), "product")
+    xo, y, p, gen = _norm_inputs((n, 2, 64, F32, F32, F32, F32, 2, 2, ALL, {}), 1)
+    _, h, _, _ = scg.residual_norm(xo, y, post=2, pre=2, **p)
+    ref, err = (f(xo.double(), y.double(), p, 2, 2)[1] for f in (R.residual_norm, R.residual_norm_error))
+    _within(h, ref, err + R.HALF[F32] * (ref.abs() + err) + R.LEAST[F32], "h")
+    assert torch.equal(scg.residual_norm(xo, y, post=2, pre=2, out_dtype=torch.int8, **p)[1], scg.quantize(h)[0])
+    dxo, dh = _randn(tuple(xo.shape), gen), _randn(tuple(xo.shape), gen)
+    _check_gradients(scg.residual_norm_backward(xo, y, dxo=dxo, dh=dh, post=2, pre=2, **p), xo, y, p, dxo, dh, 2, 2, {})
+    f, ax = scg.rope_table([64])
+    x = _randn((n, 3, 2, 64), gen)
+    pos = torch.randint(0, 1000, (n, 1, 3), generator=gen, device="cuda", dtype=torch.int32)
+    ref, mag = R.rope(x, pos, f, ax, False, False)
+    _within(scg.rope(x, pos, f, ax), ref, 8 * R.U * mag + 1e-30, "rope")
+
+
 # ---------------------------------------------------------------- together, streams, graphs
 
 def _block(scg, s):
@@ -976,6 +1030,29 @@ def test_graph_replays(scg):
         torch.cuda.synchronize()
         for n in eager:
             assert torch.equal(held[n].view(torch.uint8), eager[n].view(torch.uint8)), n
+
+
+def test_a_given_stream_in_a_graph(scg):
+    _note("a given stream in a graph")
+    gen = _gen(36)
+    A, sA = _operand((128, 8192), gen, E4, 1)
+    B, sB = _operand((128, 8192), gen, E4, 128)
+    x = _randn((500, 1152), gen)
+    want = scg.fp8_gemm(A, sA, B, sB), scg.residual_norm(x, x)[1]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        a, b = scg.fp8_gemm(A, sA, B, sB, stream=side), scg.residual_norm(x, x, stream=side)[1]
+        torch.cuda.current_stream().wait_stream(side)
+        c = a * 2
+    for _ in range(3):
+        for t in (a, b, c):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = scg.fp8_gemm(A, sA, B, sB)
+        assert torch.equal(a, eager) and torch.equal(a, want[0]) and torch.equal(b, want[1]) and torch.equal(c, want[0] * 2)
 
 
 def test_refusals_of_tensors(scg):
