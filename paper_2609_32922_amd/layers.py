@@ -106,11 +106,9 @@ def _workspace(dev, nbytes, given):
     return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
 
 
-def _unrecorded(*tensors):
-    """Refuses tensors whose gradient would be lost without a word."""
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            raise ValueError("a tensor requires a gradient, and autograd does not record this call: call it under torch.no_grad()")
+def _unrecorded():
+    """Of a call where gradients are recorded and a tensor requires one: it would be lost without a word."""
+    raise ValueError("a tensor requires a gradient, and autograd does not record this call: call it under torch.no_grad()")
 
 
 def _written(t):
@@ -168,8 +166,8 @@ def fp8_quantize(X, *, dtype=None, block: int = SC_BLOCK_1X128, stream=None):
     import torch
     if stream is not None:
         return _on_stream(stream, X.device, lambda: fp8_quantize(X, dtype=dtype, block=block))
-    if torch.is_grad_enabled():
-        _unrecorded(X)
+    if torch.is_grad_enabled() and X.requires_grad:
+        _unrecorded()
     if dtype is None:
         dtype = torch.float8_e4m3fn
     key = ("quantize", X.shape, X.stride(), X.dtype, X.device, dtype, block)
@@ -238,8 +236,9 @@ def fp8_gemm(A, sA, B, sB, *, bias=None, out=None, out_dtype=None, workspace=Non
     import torch
     if stream is not None:
         return _on_stream(stream, A.device, lambda: fp8_gemm(A, sA, B, sB, bias=bias, out=out, out_dtype=out_dtype, workspace=workspace))
-    if torch.is_grad_enabled():
-        _unrecorded(A, sA, B, sB, bias, out)
+    if torch.is_grad_enabled() and (A.requires_grad or sA.requires_grad or B.requires_grad or sB.requires_grad or
+                                    (bias is not None and bias.requires_grad) or (out is not None and out.requires_grad)):
+        _unrecorded()
     key = ("gemm", A.shape, A.stride(), A.dtype, A.device, sA.shape, sA.stride(), sA.dtype, sA.device, B.shape, B.stride(), B.dtype,
            B.device, sB.shape, sB.stride(), sB.dtype, sB.device, out_dtype, _form(bias), _form(out))
     p = _plans.get(key) or _gemm_plan(key, A, sA, B, sB, bias, out, out_dtype)
@@ -328,8 +327,11 @@ def residual_norm(x, y=None, *, post: int = SC_NORM_NONE, pre: int = SC_NORM_LAY
             x, y, post=post, pre=pre, post_weight=post_weight, post_bias=post_bias, gate=gate, pre_weight=pre_weight, pre_bias=pre_bias,
             res_scale=res_scale, post_offset=post_offset, pre_offset=pre_offset, post_eps=post_eps, pre_eps=pre_eps,
             out_dtype=out_dtype, want_x=want_x, want_h=want_h, want_rowmax=want_rowmax, inplace=inplace))
-    if torch.is_grad_enabled():
-        _unrecorded(x, y, post_weight, post_bias, gate, pre_weight, pre_bias)
+    if torch.is_grad_enabled() and (
+            x.requires_grad or (y is not None and y.requires_grad) or (post_weight is not None and post_weight.requires_grad) or
+            (post_bias is not None and post_bias.requires_grad) or (gate is not None and gate.requires_grad) or
+            (pre_weight is not None and pre_weight.requires_grad) or (pre_bias is not None and pre_bias.requires_grad)):
+        _unrecorded()
     if out_dtype is None:
         out_dtype = x.dtype
     key = ("norm", x.shape, x.stride(), x.dtype, x.device, _form(y), _form(post_weight), _form(post_bias), _form(gate),
@@ -501,8 +503,8 @@ def rope(x, pos, freq, axis, *, interleaved: bool = False, inverse: bool = False
     if stream is not None:
         return _on_stream(stream, x.device, lambda: rope(x, pos, freq, axis, interleaved=interleaved, inverse=inverse, out=out,
                                                          out_dtype=out_dtype))
-    if torch.is_grad_enabled():
-        _unrecorded(x, freq, out)
+    if torch.is_grad_enabled() and (x.requires_grad or freq.requires_grad or (out is not None and out.requires_grad)):
+        _unrecorded()
     key = ("rope", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved, inverse, out_dtype, _form(out))
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, inverse, out, out_dtype, False)
@@ -523,8 +525,8 @@ def rope_quantize(x, pos, freq, axis, *, interleaved: bool = False, want_rowmax:
     import torch
     if stream is not None:
         return _on_stream(stream, x.device, lambda: rope_quantize(x, pos, freq, axis, interleaved=interleaved, want_rowmax=want_rowmax))
-    if torch.is_grad_enabled():
-        _unrecorded(x, freq)
+    if torch.is_grad_enabled() and (x.requires_grad or freq.requires_grad):
+        _unrecorded()
     key = ("rope int8", x.shape, x.stride(), x.dtype, x.device, pos.shape, pos.stride(), pos.dtype, pos.device, freq.shape, freq.dtype,
            freq.device, axis.shape, axis.dtype, axis.device, freq.stride(), axis.stride(), interleaved)
     p = _plans.get(key) or _rope_plan(key, x, pos, freq, axis, interleaved, False, None, None, True)
