@@ -298,7 +298,8 @@ int sc_fp8_gemm_workspace_size(const sc_fp8_gemm_desc *desc, size_t *bytes);
  *   bias   fp32           bias[b*strideBias + j], NULLABLE
  *   out    typeO          out[b*strideO + i*ldo + j]   (written; K = 0 gives the bias, or 0)
  *   workspace             as sc_gemm's; NULL where sc_fp8_gemm_workspace_size gives 0
- * A large product is slower by several times where A or B starts off 16 bytes while its strides are multiples of 16.
+ * A large product takes two to four times as long where A or B starts off 16 bytes while its strides are multiples of 16
+ * (18464 x 4096 x 1024 to bfloat16: 95 and 331 us), and one of float32 or float16 results up to twice as long as one of bfloat16.
  * The order of the sums depends on sizes, types, strides and alignment alone: same call, same bits.
  */
 int sc_fp8_gemm(const sc_fp8_gemm_desc *desc, const void *A, const float *sA, const void *B, const float *sB,

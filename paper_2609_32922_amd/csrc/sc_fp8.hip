@@ -604,8 +604,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64, 2) void k_fp8_gemm(Gemm
 // Up to 16 rows: a block has 16 MI x 16 NI outputs, and its eight waves deal the
 // blocks of 128 among themselves.  A wave takes its fragments from memory as they lie (a row's 128 bytes by four lanes, 64 of
 // them at a time), the next block's while one is multiplied; the eight sums are joined in LDS in order.  Results of every type
-// take the 16-bit products (Frag): latency bounds it (1 x 4608 x 1152: 6.2 us), and the conversions hide behind it (16 x 4096 x 1024
-// 6.2 us with them and without).
+// take the 16-bit products (Frag): latency bounds it, and the conversions hide behind it but for a little (in a graph 1 x 4608 x 1152
+// 7.2 us, 6.9 by 8-bit products; 16 x 16384 x 4096 29.9 and 29.0; 16 x 65536 x 2048 69.1 and 66.5, 1.9 TB/s).
 constexpr int DW = 8;
 template <int TA, int TB, int MI, int NI>
 __global__ __launch_bounds__(64 * DW) void k_fp8_direct(GemmArgs g, uint32_t tiles) {
@@ -923,7 +923,9 @@ static hipError_t launch_gemm(const GemmArgs &g, hipStream_t st) {
         else launch_parts<TA, TB, EXACT, 2>(g, st);
     } else {
         // Microseconds by what was measured: a stage of a round of tiles and what a round costs besides (8192 x 8192 x 8192 takes
-        // 517 us in 256 x 256 tiles and 628 in 128 x 128; 4096 x 4608 x 1152 51 and 40; 18464 x 4096 x 1024 101 and 114).
+        // 532 us in 256 x 256 tiles and 716 in 128 x 128; 8192 x 4096 x 4096 151 and 189; 18464 x 4096 x 1024 104 and 118; 4096 x 4608 x 1152
+        // is the faster in 128 x 128, 40 against 51).  With a scale for each row of B both cost more, the 256 x 256 tiles spill 15 registers,
+        // and the order is the same: 647 and 816, 179 and 214, 116 and 123.
         const double big = (double)((tiles_of(g, 256) + 255) / 256) * (2.0 * g.KB + 5.6),
                      small = (double)((tiles_of(g, 128) + 511) / 512) * (1.225 * g.KB + 1.2);
         if (EXACT || small < big) {

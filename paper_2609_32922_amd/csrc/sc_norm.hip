@@ -588,7 +588,13 @@ static void backward_of(const NormArgs &a, int types, hipStream_t st) {
     else launch_backward<W, NV, 4, 4, false>(a, st);
 }
 // The fewest waves that hold a row in two quads a thread (three just below a power of two's half); gradients of more than 4096
-// elements in four, since sixteen waves have 128 registers each and spill (1024 x 8192 with both norms: 197 us, and 72 by eight)
+// elements in four, since sixteen waves have 128 registers each (1024 x 8192 with both norms: 197 us, and 72 by eight).
+// Scratch, in bytes a lane as the compiler reports it: none where everything but x has 16 bits and x too, up to 8192 elements forward,
+// and from 1537 to 4096 backward (to 8192 without a norm behind the branch).  Elsewhere it is 12 (float32 x) or 60 (float32 parameters,
+// rows off four elements) forward, where the words of a row are filled in one of two ways by the type at run time; 0 to 364 backward
+// up to 1536 elements, 0 to 128 up to 4096.  Registers spill in gradients of 1025 to 1536 elements with a norm behind the branch and
+// a float32 operand or rows off four elements (11 to 182), of 4097 to 8192 with such a norm (140 to 428) or such an operand or rows (21 to 173),
+// and in both directions past 8192.
 static hipError_t launch_rows(const NormArgs &a, bool back, bool vec, hipStream_t st) {
     const bool x16 = a.typeX != SC_F32, rest16 = (a.y == nullptr || a.typeY != SC_F32) && a.typeP != SC_F32 && (!back || a.dh == nullptr || a.typeH != SC_F32);
     const int types = !vec ? ODD : x16 && rest16 ? ALL_16 : rest16 ? ANY_16 : ANY_ANY, D = a.D;

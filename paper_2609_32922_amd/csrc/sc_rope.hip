@@ -82,8 +82,8 @@ struct Eight {
 };
 
 // A thread has four pairs of a token (or eight elements that pass) and takes them through a.each heads with one set of cosines,
-// HEADS of them at a time, the next ones' loads in flight.  Memory-bound (24960 x 24 x 128 in 16 bits: 60 us,
-// 5.1 TB/s).  VEC: rows, pairs and halves on four elements.
+// HEADS of them at a time, the next ones' loads in flight.  Memory-bound (24960 x 24 x 128 in 16 bits: 61 us,
+// 5.0 TB/s).  VEC: rows, pairs and halves on four elements.
 // STREAM: stores that do not stay in the caches.
 constexpr int HEADS = 4;
 template <bool VEC, bool NEAR, int R, bool STREAM, bool INT8>
