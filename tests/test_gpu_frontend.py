@@ -300,7 +300,7 @@ def test_binding_memory_of_a_given_stream(dev):
         got = scg.gemm(q, s, q, s, L, L_max=32, seed=3, workspace=ws)[0]
     ws = None
     t = torch.empty(size, dtype=torch.uint8, device=dev)
-    assert t.data_ptr() != first
+    assert t.data_ptr() != first or side.query()        # (once all is done there it may be given away)
     t.fill_(0x3C)
     torch.cuda.synchronize()
     assert torch.equal(got, want[0])

@@ -971,7 +971,7 @@ def test_workspace_of_another_stream(scg):
                 two = want[1]
                 ws = None
             t = torch.empty(first[1], dtype=torch.uint8, device="cuda")
-            assert t.data_ptr() != first[0]
+            assert t.data_ptr() != first[0] or side.query()          # (once all is done there it may be given away)
             t.fill_(0x3C)
             torch.cuda.synchronize()
             assert torch.equal(one, want[0]) and torch.equal(two, want[1])
